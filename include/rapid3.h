@@ -259,6 +259,77 @@ int rapid3_gated_step_host(rapid3_ctx* ctx, const void* q_host, const void* k_ho
 int rapid3_cache_step(const void* x, void* o, void* delta, const int32_t* action_host, int B,
                       int64_t elems_per_image, void* stream);
 
+/*
+ * Rotary positions of Q and K heads, alone or behind the RMS normalisation of each head: the producer of
+ * rapid3_gated_step_fused on its own, for any [B, H, N, D] strides, types and shared key heads, with its gradient.
+ * No context; asynchronous on `stream`, one launch (rapid3_norm_rotary_backward: two), nothing is allocated.
+ *
+ * Row x[D] of sequence b, token n, with coordinates pos[b][n][axis]; channel pair i (i < channels / 2) is
+ *   RAPID3_TURN_PAIRS:  (2 i, 2 i + 1)        RAPID3_TURN_HALVES: (i, i + channels / 2)
+ * and turns by the angle pos * freq[i], whose axis is the first a with i < axis_pairs[0] + .. + axis_pairs[a]:
+ *   z_first = amplitude (y_first cos - y_second sin),  z_second = amplitude (y_first sin + y_second cos);
+ * channels from `channels` on are copied.  y = x, or x / sqrt(mean(x^2) + eps) * gain in the norm calls.  fp32 arithmetic
+ * (angles fp64), rounded once to the tensors' type.  Outputs may be the inputs (in place); they may not overlap otherwise.
+ */
+enum { RAPID3_BF16 = 0, RAPID3_F16 = 1, RAPID3_F32 = 2 };
+enum { RAPID3_TURN_PAIRS = 0, RAPID3_TURN_HALVES = 1 };
+
+/* A tensor [B, H, N, D], D stride 1.  Strides in elements; of dimensions with more than one entry they are at least D and
+ * keep rows 16-byte aligned, as is `data`. */
+typedef struct rapid3_rows {
+    void* data;                              /* device */
+    int64_t stride_b, stride_h, stride_n;
+} rapid3_rows;
+
+typedef struct rapid3_heads {
+    int32_t type;                            /* RAPID3_BF16, RAPID3_F16 or RAPID3_F32, of all tensors  */
+    int32_t B, N, D;                         /* D: a multiple of 16, 16..256; B * N < 2^31             */
+    int32_t H_q, H_k;                        /* heads of Q and of K; H_k = 0: there is no K (NULL)     */
+} rapid3_heads;
+
+typedef struct rapid3_turn {
+    int32_t layout;                          /* RAPID3_TURN_PAIRS or RAPID3_TURN_HALVES                                   */
+    int32_t channels;                        /* turned channels, the first of a head: even, 0..D (HALVES: a multiple of 8) */
+    int32_t axes;                            /* coordinates of a position, 1..4                                            */
+    int32_t axis_pairs[4];                   /* pairs that each turns; their sum is channels / 2                           */
+    const double* freq;                      /* device [channels / 2], radians per position                                */
+    const int32_t* pos;                      /* device; pos[b * pos_stride_b + n * pos_stride_n + axis], or NULL: pos0 + n */
+    int64_t pos_stride_b, pos_stride_n;      /* >= 0; pos_stride_b 0: the same positions in every sequence                 */
+    int32_t pos0;                            /* 0..2^30                                                                    */
+    float amplitude;
+} rapid3_turn;
+
+/* The rotation alone.  backward != 0: the gradient of its input from that of its output (the transposed rotation). */
+int rapid3_rotary(const rapid3_heads* shape, const rapid3_rows* q, const rapid3_rows* k, const rapid3_turn* turn, int backward,
+                  const rapid3_rows* q_out, const rapid3_rows* k_out, void* stream);
+
+/* Normalisation, gain and rotation in one pass.  q_gain, k_gain: device fp32 [D]; eps >= 0. */
+int rapid3_norm_rotary(const rapid3_heads* shape, const rapid3_rows* q, const rapid3_rows* k, const float* q_gain, const float* k_gain,
+                       float eps, const rapid3_turn* turn, const rapid3_rows* q_out, const rapid3_rows* k_out, void* stream);
+
+/* Its gradients: from dq_out, dk_out (of its outputs) and q, k (its inputs) to dq, dk (which may be dq_out, dk_out or q, k) and
+ * dq_gain, dk_gain (device fp32 [D], overwritten).  workspace: device, 16-byte aligned, of at least the bytes that
+ * rapid3_norm_rotary_workspace_bytes gives for the shape, used by one call at a time; nothing in it has to be set.  The sums over
+ * rows are taken in a fixed order: the same call gives the same bits. */
+int rapid3_norm_rotary_backward(const rapid3_heads* shape, const rapid3_rows* dq_out, const rapid3_rows* dk_out, const rapid3_rows* q,
+                                const rapid3_rows* k, const float* q_gain, const float* k_gain, float eps, const rapid3_turn* turn,
+                                const rapid3_rows* dq, const rapid3_rows* dk, float* dq_gain, float* dk_gain, void* workspace,
+                                int64_t workspace_bytes, void* stream);
+int64_t rapid3_norm_rotary_workspace_bytes(const rapid3_heads* shape);
+
+/*
+ * Frequencies of rotary positions, base^(-2 i / channels), and their scalings for contexts `factor` times longer than the
+ * `trained` one (host arithmetic, fp64; freq_host [channels / 2]):
+ *   RAPID3_SCALE_LINEAR  every frequency divided by factor;
+ *   RAPID3_SCALE_BASE    the base multiplied by factor^(channels / (channels - 2)): the slowest pair is divided by factor, the
+ *                        fastest one keeps its frequency;
+ *   RAPID3_SCALE_PARTS   by how often a pair turns over the trained length, t = trained * f / 2 pi: f * s + f / factor * (1 - s) with
+ *                        s = clamp((t - slow_turns) / (fast_turns - slow_turns), 0, 1); *amplitude = 1 + 0.1 ln(factor), else 1.
+ */
+enum { RAPID3_SCALE_NONE = 0, RAPID3_SCALE_LINEAR = 1, RAPID3_SCALE_BASE = 2, RAPID3_SCALE_PARTS = 3 };
+int rapid3_rotary_freqs(int channels, double base, int scaling, double factor, int trained, double fast_turns, double slow_turns,
+                        double* freq_host, float* amplitude);
+
 /* Device pointers of the workspace rapid3_gated_step fills (any may be NULL): layouts as in
  * rapid3_block_scores / rapid3_select_mask with n_img = number of sparse images of the last step. */
 int rapid3_workspace(rapid3_ctx* ctx, float** scores, uint64_t** bitmask, int32_t** kept_idx,

@@ -25,6 +25,7 @@ EXPORTS = [
     "rapid3_gated_step_host", "rapid3_workspace", "rapid3_launch_count", "rapid3_last_status",
     "rapid3_profile", "rapid3_profile_read", "rapid3_block_scores_static", "rapid3_static_scratch_bytes", "rapid3_cache_step", "rapid3_gated_step_device", "rapid3_gated_step_heads", "rapid3_equivalent_steps", "rapid3_select_mask_mass", "rapid3_gated_step_fused", "rapid3_gated_step_mass",
     "rapid3_debug_inject_timeout",
+    "rapid3_rotary", "rapid3_norm_rotary", "rapid3_norm_rotary_backward", "rapid3_norm_rotary_workspace_bytes", "rapid3_rotary_freqs",
 ]
 
 
@@ -38,6 +39,20 @@ class Shape(ctypes.Structure):
     _fields_ = [("B_max", ctypes.c_int32), ("H", ctypes.c_int32), ("D", ctypes.c_int32),
                 ("n_text", ctypes.c_int32), ("n_image", ctypes.c_int32), ("block", ctypes.c_int32),
                 ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_n", ctypes.c_int64)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_n", ctypes.c_int64)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("type", "B", "N", "D", "H_q", "H_k")]
+
+
+class Turn(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("channels", ctypes.c_int32), ("axes", ctypes.c_int32), ("axis_pairs", ctypes.c_int32 * 4),
+                ("freq", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("pos_stride_b", ctypes.c_int64), ("pos_stride_n", ctypes.c_int64),
+                ("pos0", ctypes.c_int32), ("amplitude", ctypes.c_float)]
 
 
 _lib = None
@@ -83,6 +98,13 @@ def load() -> ctypes.CDLL:
     lib.rapid3_equivalent_steps.argtypes = [i32p, f32p, f32p, ci, ctypes.POINTER(ctypes.c_double), i64p]
     lib.rapid3_cache_step.argtypes = [vp, vp, vp, i32p, ci, ctypes.c_int64, vp]
     lib.rapid3_static_scratch_bytes.restype = ctypes.c_int64
+    rows, heads, turn = ctypes.POINTER(Rows), ctypes.POINTER(Heads), ctypes.POINTER(Turn)
+    lib.rapid3_rotary.argtypes = [heads, rows, rows, turn, ci, rows, rows, vp]
+    lib.rapid3_norm_rotary.argtypes = [heads, rows, rows, vp, vp, cf, turn, rows, rows, vp]
+    lib.rapid3_norm_rotary_backward.argtypes = [heads, rows, rows, rows, rows, vp, vp, cf, turn, rows, rows, vp, vp, vp, ctypes.c_int64, vp]
+    lib.rapid3_norm_rotary_workspace_bytes.argtypes = [heads]
+    lib.rapid3_norm_rotary_workspace_bytes.restype = ctypes.c_int64
+    lib.rapid3_rotary_freqs.argtypes = [ci, ctypes.c_double, ci, ctypes.c_double, ci, ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double), f32p]
     _lib = lib
     return lib
 
@@ -323,6 +345,135 @@ def rapid3_cache_step(x: torch.Tensor, o: torch.Tensor, delta: torch.Tensor, act
     elems = x[0].numel()
     _check(load().rapid3_cache_step(_ptr(x), _ptr(o), _ptr(delta), _i32(actions), B, elems, _stream()),
            "rapid3_cache_step")
+
+
+_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _rows(t: Optional[torch.Tensor]):
+    if t is None:
+        return None
+    sb, sh, sn, _ = t.stride()
+    return Rows(t.data_ptr(), sb, sh, sn)
+
+
+def _check_tensors(what: str, like: torch.Tensor, tensors):
+    """Each (name, tensor, shape): on `like`'s device, which is the current one, of its type and that shape, channels adjacent."""
+    if not like.is_cuda or like.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{what}: tensors must be on the current CUDA device")
+    for name, t, shape in tensors:
+        if t is None or t.dtype != like.dtype or t.device != like.device or t.shape != shape or (t.stride(-1) != 1 and shape[-1] > 1):
+            raise ValueError(f"{what}: {name} must be {tuple(shape)} of {like.dtype} on {like.device} with adjacent channels")
+
+
+def _check_vector(what: str, name: str, t: Optional[torch.Tensor], n: int, like: torch.Tensor, dtype=torch.float32):
+    if t is None or t.dtype != dtype or t.device != like.device or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be {n} contiguous values of {dtype} on {like.device}")
+
+
+def rapid3_rotary_freqs(channels: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: int = 1,
+                        fast_turns: float = 32.0, slow_turns: float = 1.0):
+    """Radians per position of channels / 2 pairs (fp64, on the host) and the amplitude; scaling: "none", "linear", "base", "parts"."""
+    freq, amplitude = torch.empty(max(0, channels) // 2, dtype=torch.float64), ctypes.c_float(0.0)
+    kind = {"none": 0, "linear": 1, "base": 2, "parts": 3}.get(scaling, -1)
+    _check(load().rapid3_rotary_freqs(int(channels), float(base), kind, float(factor), int(trained), float(fast_turns), float(slow_turns),
+                                      ctypes.cast(freq.data_ptr(), ctypes.POINTER(ctypes.c_double)), ctypes.byref(amplitude)), "rapid3_rotary_freqs")
+    return freq, amplitude.value
+
+
+class Rotary:
+    """How positions turn the heads of rapid3_rotary and rapid3_norm_rotary: made once, used for any number of calls.
+
+    layout      "pairs": channels (2 i, 2 i + 1) turn together; "halves": (i, i + channels / 2)
+    freq        fp64 [channels / 2] on the GPU, radians per position (see rapid3_rotary_freqs)
+    pos         int32 [B or 1, N, axes] on the GPU, read when the kernels run; None: pos0 + n
+    axis_pairs  how many pairs each coordinate turns, in order; None: the first turns all
+    """
+
+    def __init__(self, layout: str, freq: torch.Tensor, pos: Optional[torch.Tensor] = None, pos0: int = 0, amplitude: float = 1.0,
+                 axis_pairs: Optional[Sequence[int]] = None):
+        if layout not in ("pairs", "halves"):
+            raise ValueError("Rotary: layout must be 'pairs' or 'halves'")
+        if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or not freq.is_cuda:
+            raise ValueError("Rotary: freq must be a contiguous fp64 vector on the GPU")
+        axes = 1 if pos is None else pos.shape[-1]
+        if pos is not None and (pos.dtype != torch.int32 or pos.dim() != 3 or pos.device != freq.device or not 1 <= axes <= 4 or
+                                (pos.stride(-1) != 1 and axes > 1)):
+            raise ValueError("Rotary: pos must be int32 [B or 1, N, axes], 1 to 4 axes, adjacent, beside freq")
+        pairs = [freq.numel()] if axis_pairs is None else [int(x) for x in axis_pairs]
+        if len(pairs) > axes or sum(pairs) != freq.numel() or min(pairs) < 0:
+            raise ValueError("Rotary: axis_pairs must be one count for each axis, freq's length in all")
+        pairs += [0] * (4 - len(pairs))
+        self.freq, self.pos, self.device = freq, pos, freq.device
+        self.B, self.N = (0, 0) if pos is None else pos.shape[:2]
+        self.turn = Turn(0 if layout == "pairs" else 1, 2 * freq.numel(), axes, (ctypes.c_int32 * 4)(*pairs), freq.data_ptr(), _ptr(pos),
+                         0 if pos is None or self.B == 1 else pos.stride(0), 0 if pos is None or self.N == 1 else pos.stride(1), int(pos0),
+                         float(amplitude))
+
+    def check(self, what: str, like: torch.Tensor):
+        B, _, N, _ = like.shape
+        if self.device != like.device or (self.pos is not None and (self.N != N or self.B not in (1, B))):
+            raise ValueError(f"{what}: the positions are those of {self.B} x {self.N} tokens on {self.device}, not of {B} x {N} on {like.device}")
+
+
+def _heads(what: str, q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, others):
+    """The shape of Q and K (k may be None), after checking them and `others`, (name, tensor, which of the two it is like)."""
+    if q.dim() != 4 or q.dtype not in _TYPES or (k is not None and (k.dim() != 4 or k.shape[0] != q.shape[0] or k.shape[2:] != q.shape[2:])):
+        raise ValueError(f"{what}: q and k must be [B, H, N, D] of bf16, fp16 or fp32 and differ in H only")
+    rotary.check(what, q)
+    _check_tensors(what, q, [("q", q, q.shape)] + ([] if k is None else [("k", k, k.shape)]) +
+                   [(name, t, (q if w == 0 else k).shape) for name, t, w in others if w == 0 or k is not None])
+    return Heads(_TYPES[q.dtype], q.shape[0], q.shape[2], q.shape[3], q.shape[1], 0 if k is None else k.shape[1])
+
+
+def rapid3_rotary(q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, q_out: Optional[torch.Tensor] = None,
+                  k_out: Optional[torch.Tensor] = None, backward: bool = False):
+    """Turns Q and K heads ([B, H, N, D], any heads each; k may be None) by their positions; outputs may be the inputs.
+    backward: q and k are gradients of the outputs, and those of the inputs come back."""
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
+    shape = _heads("rapid3_rotary", q, k, rotary, (("q_out", q_out, 0), ("k_out", k_out, 1)))
+    _check(load().rapid3_rotary(shape, _rows(q), _rows(k), rotary.turn, int(backward), _rows(q_out), None if k is None else _rows(k_out), _stream()),
+           "rapid3_rotary")
+    return q_out, k_out
+
+
+def rapid3_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_gain: torch.Tensor, k_gain: Optional[torch.Tensor], eps: float,
+                       rotary: Rotary, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """RMS normalisation of each head, gain (fp32 [D]) and rotation in one pass; outputs may be the inputs."""
+    what = "rapid3_norm_rotary"
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
+    shape = _heads(what, q, k, rotary, (("q_out", q_out, 0), ("k_out", k_out, 1)))
+    _check_vector(what, "q_gain", q_gain, q.shape[3], q)
+    if k is not None:
+        _check_vector(what, "k_gain", k_gain, q.shape[3], q)
+    _check(load().rapid3_norm_rotary(shape, _rows(q), _rows(k), _ptr(q_gain), _ptr(k_gain), float(eps), rotary.turn, _rows(q_out),
+                                     None if k is None else _rows(k_out), _stream()), what)
+    return q_out, k_out
+
+
+def rapid3_norm_rotary_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q: torch.Tensor, k: Optional[torch.Tensor],
+                                q_gain: torch.Tensor, k_gain: Optional[torch.Tensor], eps: float, rotary: Rotary,
+                                dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                                dq_gain: Optional[torch.Tensor] = None, dk_gain: Optional[torch.Tensor] = None):
+    """Gradients of rapid3_norm_rotary's inputs and gains from those of its outputs; q and k are its inputs.
+    dq and dk may be dq_out and dk_out.  The same call gives the same bits."""
+    what = "rapid3_norm_rotary_backward"
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None and k is not None else dk
+    dq_gain = torch.empty_like(q_gain) if dq_gain is None else dq_gain
+    dk_gain = torch.empty_like(k_gain) if dk_gain is None and k is not None and k_gain is not None else dk_gain
+    shape = _heads(what, q, k, rotary, (("dq_out", dq_out, 0), ("dk_out", dk_out, 1), ("dq", dq, 0), ("dk", dk, 1)))
+    for name, t in (("q_gain", q_gain), ("dq_gain", dq_gain)) + ((("k_gain", k_gain), ("dk_gain", dk_gain)) if k is not None else ()):
+        _check_vector(what, name, t, q.shape[3], q)
+    lib = load()
+    size = lib.rapid3_norm_rotary_workspace_bytes(shape)
+    workspace = torch.empty(max(16, size), dtype=torch.uint8, device=q.device)
+    _check(lib.rapid3_norm_rotary_backward(shape, _rows(dq_out), None if k is None else _rows(dk_out), _rows(q), _rows(k), _ptr(q_gain),
+                                           _ptr(k_gain), float(eps), rotary.turn, _rows(dq), None if k is None else _rows(dk), _ptr(dq_gain),
+                                           None if k is None else _ptr(dk_gain), _ptr(workspace), size, _stream()), what)
+    return dq, dk, dq_gain, dk_gain
 
 
 def static_scratch_bytes() -> int:
