@@ -330,6 +330,49 @@ enum { RAPID3_SCALE_NONE = 0, RAPID3_SCALE_LINEAR = 1, RAPID3_SCALE_BASE = 2, RA
 int rapid3_rotary_freqs(int channels, double base, int scaling, double factor, int trained, double fast_turns, double slow_turns,
                         double* freq_host, float* amplitude);
 
+/*
+ * Attention with a sliding window and first tokens that stay visible: the static pattern of near tokens beside the block-sparse
+ * one, for prompts, single tokens against a cache, and training.  Row i of sequence b stands at position p = i + kv_len[b] - q_len[b]
+ * (the rows are the sequence's last) and sees key j < kv_len[b] if and only if
+ *     j <= p + right  and  (j >= p - left  or  j < n_sink),      or      0 <= p < n_full
+ * (a bound of -1 is none).  right = 0: causal.  left = right, n_sink = n_full = text tokens: joint attention whose image tokens
+ * see the text and their neighbours in raster order, and whose text tokens see everything.
+ *     out = softmax(softmax_scale q k over the visible keys) v,   lse = log sum exp(softmax_scale q k) (natural, fp32)
+ * A row that sees no key gets zeros and lse = -inf.  Scores, softmax and sums are fp32, the weights are rounded to the tensors' type
+ * for the product with V.  Query head h reads key head h / (H / H_kv).
+ * No context and, but for the backward pass's, no workspace; asynchronous on `stream`; nothing is allocated; one launch (backward: three).
+ * Rows from q_len[b] on are neither read nor written, keys from kv_len[b] on do not count: what lies there may be anything.  Other
+ * non-finite inputs give undefined results.
+ */
+typedef struct rapid3_window {
+    int32_t type;                            /* RAPID3_BF16 or RAPID3_F16, of all tensors                      */
+    int32_t B, H, H_kv, D;                   /* H a multiple of H_kv, up to 65535; D 64 or 128                 */
+    int32_t n_q, n_kv;                       /* places of a sequence in Q and in K, V; >= 1, below 2^30 - 1    */
+    int32_t left, right;                     /* >= 0, or -1 for no bound                                       */
+    int32_t n_sink, n_full;                  /* >= 0                                                           */
+    float softmax_scale;                     /* > 0, finite                                                    */
+    const int32_t* q_len;                    /* device [B], or NULL: n_q; taken into 0..n_q                    */
+    const int32_t* kv_len;                   /* device [B], or NULL: n_kv; taken into 0..n_kv                  */
+} rapid3_window;
+
+/* q, out [B, H, n_q, D]; k, v [B, H_kv, n_kv, D]; lse fp32 [B][H][n_q] or NULL.  out may not overlap the inputs.
+ * Where H / H_kv * n_q is 16 or less, one kernel reads each visible key once for all query heads that share it. */
+int rapid3_window_attn(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, const rapid3_rows* v, const rapid3_rows* out, float* lse,
+                       void* stream);
+
+/* Gradients dq, dk, dv from dout and what rapid3_window_attn read and wrote (lse is needed).  Outputs overlap nothing.  Keys that no
+ * row sees get zeros; rows from q_len[b] on and keys from kv_len[b] on are left as they were.  B * H <= 65535.  workspace: device, 16-byte
+ * aligned, of at least the bytes that rapid3_window_workspace_bytes gives, used by one call at a time; nothing in it has to be set.  The
+ * sums are taken in a fixed order: the same call gives the same bits. */
+int rapid3_window_attn_backward(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, const rapid3_rows* v, const rapid3_rows* out,
+                                const float* lse, const rapid3_rows* dout, const rapid3_rows* dq, const rapid3_rows* dk, const rapid3_rows* dv,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+int64_t rapid3_window_workspace_bytes(const rapid3_window* w);
+
+/* The current device's status word of the two calls above (RAPID3_OK, or RAPID3_ERR_TIMEOUT after a bounded wait inside a kernel ran
+ * out, whose results are then incomplete); clears it.  Synchronises the device. */
+int rapid3_window_status(int* status);
+
 /* Device pointers of the workspace rapid3_gated_step fills (any may be NULL): layouts as in
  * rapid3_block_scores / rapid3_select_mask with n_img = number of sparse images of the last step. */
 int rapid3_workspace(rapid3_ctx* ctx, float** scores, uint64_t** bitmask, int32_t** kept_idx,

@@ -26,6 +26,7 @@ EXPORTS = [
     "rapid3_profile", "rapid3_profile_read", "rapid3_block_scores_static", "rapid3_static_scratch_bytes", "rapid3_cache_step", "rapid3_gated_step_device", "rapid3_gated_step_heads", "rapid3_equivalent_steps", "rapid3_select_mask_mass", "rapid3_gated_step_fused", "rapid3_gated_step_mass",
     "rapid3_debug_inject_timeout",
     "rapid3_rotary", "rapid3_norm_rotary", "rapid3_norm_rotary_backward", "rapid3_norm_rotary_workspace_bytes", "rapid3_rotary_freqs",
+    "rapid3_window_attn", "rapid3_window_attn_backward", "rapid3_window_workspace_bytes", "rapid3_window_status",
 ]
 
 
@@ -53,6 +54,11 @@ class Turn(ctypes.Structure):
     _fields_ = [("layout", ctypes.c_int32), ("channels", ctypes.c_int32), ("axes", ctypes.c_int32), ("axis_pairs", ctypes.c_int32 * 4),
                 ("freq", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("pos_stride_b", ctypes.c_int64), ("pos_stride_n", ctypes.c_int64),
                 ("pos0", ctypes.c_int32), ("amplitude", ctypes.c_float)]
+
+
+class Window(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("type", "B", "H", "H_kv", "D", "n_q", "n_kv", "left", "right", "n_sink", "n_full")] + [
+        ("softmax_scale", ctypes.c_float), ("q_len", ctypes.c_void_p), ("kv_len", ctypes.c_void_p)]
 
 
 _lib = None
@@ -104,6 +110,12 @@ def load() -> ctypes.CDLL:
     lib.rapid3_norm_rotary_backward.argtypes = [heads, rows, rows, rows, rows, vp, vp, cf, turn, rows, rows, vp, vp, vp, ctypes.c_int64, vp]
     lib.rapid3_norm_rotary_workspace_bytes.argtypes = [heads]
     lib.rapid3_norm_rotary_workspace_bytes.restype = ctypes.c_int64
+    win = ctypes.POINTER(Window)
+    lib.rapid3_window_attn.argtypes = [win, rows, rows, rows, rows, vp, vp]
+    lib.rapid3_window_attn_backward.argtypes = [win, rows, rows, rows, rows, vp, rows, rows, rows, rows, vp, ctypes.c_int64, vp]
+    lib.rapid3_window_workspace_bytes.argtypes = [win]
+    lib.rapid3_window_workspace_bytes.restype = ctypes.c_int64
+    lib.rapid3_window_status.argtypes = [ctypes.POINTER(ci)]
     lib.rapid3_rotary_freqs.argtypes = [ci, ctypes.c_double, ci, ctypes.c_double, ci, ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double), f32p]
     _lib = lib
     return lib
@@ -474,6 +486,65 @@ def rapid3_norm_rotary_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Ten
                                            _ptr(k_gain), float(eps), rotary.turn, _rows(dq), None if k is None else _rows(dk), _ptr(dq_gain),
                                            None if k is None else _ptr(dk_gain), _ptr(workspace), size, _stream()), what)
     return dq, dk, dq_gain, dk_gain
+
+
+def _window(what: str, q: torch.Tensor, k: torch.Tensor, others, left: int, right: int, n_sink: int, n_full: int,
+            q_len: Optional[torch.Tensor], kv_len: Optional[torch.Tensor], softmax_scale: Optional[float]):
+    """The shape and rule of a windowed attention, after checking Q, K, the lengths and `others`, (name, tensor, which of the two it is like)."""
+    if q.dim() != 4 or k.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float16) or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
+        raise ValueError(f"{what}: q [B, H, n_q, D] and k [B, H_kv, n_kv, D] must be bf16 or fp16 and agree in B and D")
+    _check_tensors(what, q, [("q", q, q.shape), ("k", k, k.shape)] + [(name, t, (q if w == 0 else k).shape) for name, t, w in others])
+    for name, t in (("q_len", q_len), ("kv_len", kv_len)):
+        if t is not None:
+            _check_vector(what, name, t, q.shape[0], q, torch.int32)
+    return Window(_TYPES[q.dtype], q.shape[0], q.shape[1], k.shape[1], q.shape[3], q.shape[2], k.shape[2], int(left), int(right), int(n_sink),
+                  int(n_full), float(softmax_scale if softmax_scale is not None else q.shape[3] ** -0.5), _ptr(q_len), _ptr(kv_len))
+
+
+def _check_lse(what: str, lse: Optional[torch.Tensor], q: torch.Tensor):
+    if lse is None or lse.dtype != torch.float32 or lse.device != q.device or lse.shape != q.shape[:3] or not lse.is_contiguous():
+        raise ValueError(f"{what}: lse must be contiguous fp32 {tuple(q.shape[:3])} on {q.device}")
+
+
+def rapid3_window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                       left: int = -1, right: int = -1, n_sink: int = 0, n_full: int = 0, q_len: Optional[torch.Tensor] = None,
+                       kv_len: Optional[torch.Tensor] = None, softmax_scale: Optional[float] = None):
+    """Attention of q [B, H, n_q, D] over k, v [B, H_kv, n_kv, D]: row i, at position p = i + kv_len - q_len, sees key j if j <= p + right and
+    (j >= p - left or j < n_sink), or if 0 <= p < n_full; -1: no bound.  q_len, kv_len: int32 [B] on the GPU, read when the kernels run.
+    Returns out (allocated, rows from q_len on unset, unless given) and lse (filled if given)."""
+    what = "rapid3_window_attn"
+    out = torch.empty_like(q) if out is None else out
+    shape = _window(what, q, k, (("v", v, 1), ("out", out, 0)), left, right, n_sink, n_full, q_len, kv_len, softmax_scale)
+    if lse is not None:
+        _check_lse(what, lse, q)
+    _check(load().rapid3_window_attn(shape, _rows(q), _rows(k), _rows(v), _rows(out), _ptr(lse), _stream()), what)
+    return out, lse
+
+
+def rapid3_window_attn_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                                dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                                left: int = -1, right: int = -1, n_sink: int = 0, n_full: int = 0, q_len: Optional[torch.Tensor] = None,
+                                kv_len: Optional[torch.Tensor] = None, softmax_scale: Optional[float] = None):
+    """Gradients of rapid3_window_attn from dout and what that call read and wrote, with the same rule, lengths and scale.
+    Rows from q_len and keys from kv_len on are left as they were.  The same call gives the same bits."""
+    what = "rapid3_window_attn_backward"
+    dq, dk, dv = (torch.empty_like(x) if g is None else g for x, g in ((q, dq), (k, dk), (v, dv)))
+    shape = _window(what, q, k, (("v", v, 1), ("out", out, 0), ("dout", dout, 0), ("dq", dq, 0), ("dk", dk, 1), ("dv", dv, 1)), left, right, n_sink,
+                    n_full, q_len, kv_len, softmax_scale)
+    _check_lse(what, lse, q)
+    lib = load()
+    size = lib.rapid3_window_workspace_bytes(shape)
+    workspace = torch.empty(max(16, size), dtype=torch.uint8, device=q.device)
+    _check(lib.rapid3_window_attn_backward(shape, _rows(q), _rows(k), _rows(v), _rows(out), _ptr(lse), _rows(dout), _rows(dq), _rows(dk), _rows(dv),
+                                           _ptr(workspace), size, _stream()), what)
+    return dq, dk, dv
+
+
+def rapid3_window_status() -> int:
+    """The current device's status word of the windowed attention, and clears it; synchronises the device."""
+    v = ctypes.c_int(0)
+    _check(load().rapid3_window_status(ctypes.byref(v)), "rapid3_window_status")
+    return v.value
 
 
 def static_scratch_bytes() -> int:

@@ -113,8 +113,8 @@ __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constan
             if (pair < half) {
                 int axis = 0;
                 while (axis + 1 < p.turn.axes && pair >= p.turn.axis_end[axis]) ++axis;
-                const int at = p.turn.pos ? __ldg(p.turn.pos + b * p.turn.pos_b + (n0 + t) * p.turn.pos_n + axis) : p.turn.pos0 + n0 + t;
-                double turns = (double)at * (__ldg(p.turn.freq + pair) * 0.15915494309189533577);
+                const int at = p.turn.pos ? __ldcg(p.turn.pos + b * p.turn.pos_b + (n0 + t) * p.turn.pos_n + axis) : p.turn.pos0 + n0 + t;
+                double turns = (double)at * (__ldcg(p.turn.freq + pair) * 0.15915494309189533577);
                 turns -= rint(turns);
                 sincospif(2.f * (float)turns, &sine, &cosine);
                 sine *= p.turn.amplitude;
@@ -137,8 +137,8 @@ __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constan
             if (NORM && here) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    ga[i] = __ldg(t.gain + (HALVES ? at0 + i : at0 + 2 * i));
-                    gb[i] = __ldg(t.gain + (HALVES ? at1 + i : at0 + 2 * i + 1));
+                    ga[i] = __ldcg(t.gain + (HALVES ? at0 + i : at0 + 2 * i));
+                    gb[i] = __ldcg(t.gain + (HALVES ? at1 + i : at0 + 2 * i + 1));
                 }
             }
             const char* in = t.in + b * t.in_b + (long long)h0 * t.in_h + (long long)n0 * t.in_n;

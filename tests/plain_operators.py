@@ -58,7 +58,7 @@ def visible(rows, keys, left, right, n_sink, n_full, q_len, kv_len, device="cpu"
             near = (j >= p - left) | (j < n_sink)
         if right >= 0:
             near = near & (j <= p + right)
-        seen[i] = (near | (p < n_full)) & (j < kv_len)
+        seen[i] = (near | (0 <= p < n_full)) & (j < kv_len)
     return seen
 
 
