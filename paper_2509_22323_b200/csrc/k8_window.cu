@@ -25,6 +25,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "window.cuh"
 
@@ -53,8 +54,11 @@ struct Params {
     float* lse;
     int H, H_kv, group;
     int mode;                                            // 0: two heads, 1: 256 rows, 2: one tile
-    int heads, row_tiles, units;                         // (sequence, head) pairs or pairs of heads; tiles of rows; their product
-    bool last_first;                                     // the last rows have the most keys
+    int heads, row_tiles;                                // (sequence, head) pairs or pairs of heads; tiles of rows
+    // The order: tiles of full rows, the longest, of all heads; then head by head, whose units share K and V in the L2 (with the heads
+    // fastest 24 heads of 4608 tokens took 220 instead of 2xx us, dense); the last rows first where these have the most keys.
+    int full_tiles;
+    bool last_first;
     float scale_log2;
 };
 
@@ -68,6 +72,19 @@ struct Cfg {
     static constexpr int O_COL = 64 * NBUF;
 };
 
+// A unit of work, written by the warp that takes it over: its index arithmetic is in no other role's way.
+struct Unit {
+    int n;                                               // key blocks; -1: no more units
+    int b, hk, head[2], row0[2], rows, keys;             // row0 >= rows: nothing for that tile
+    Blocks all;
+    // of the unit's list of blocks a tile uses the first ones and those from `from` on, so many (0, 0: none)
+    int first[2], from[2], count[2];
+    // of a softmax warp's rows: see bounds_of
+    int4 bounds[SOFTMAX_WARPS];
+    int2 free[SOFTMAX_WARPS];
+    __device__ __forceinline__ int tiles() const { return first[1] + count[1] > 0 ? 2 : 1; }
+};
+
 struct __align__(16) Ctl {
     uint4 taken;
     unsigned long long taken_full, near_end, tail_full;
@@ -79,21 +96,18 @@ struct __align__(16) Ctl {
     unsigned long long pv_done[2][2], o_done[2], drain[2];
     uint32_t tmem_base;
     volatile int abort_flag;
-    int unit[2];
+    Unit unit[2];
 };
 template <int D>
 constexpr size_t smem_bytes() { return (size_t)Cfg<D>::DATA_BYTES + sizeof(Ctl) + 1024; }
 
-// A unit of work as every role derives it from its number.
-struct Unit {
-    int b, hk, head[2], row0[2], rows, keys;             // row0 >= rows: nothing for that tile
-    Blocks tile[2], all;
-    int n;
-};
 __device__ __forceinline__ Unit unit_of(const Params& p, int L) {
     Unit u;
-    int rt = L / p.heads, x = L - rt * p.heads;
-    if (p.last_first) rt = p.row_tiles - 1 - rt;
+    const int full = p.full_tiles * p.heads, tiles = L < full ? p.full_tiles : p.row_tiles - p.full_tiles;
+    const int y = L < full ? L : L - full, x = y / tiles;
+    int rt = y - x * tiles;
+    if (p.last_first) rt = tiles - 1 - rt;
+    if (L >= full) rt += p.full_tiles;
     if (p.mode == 0) {
         const int pairs = p.H / 2;
         u.b = x / pairs;
@@ -104,17 +118,51 @@ __device__ __forceinline__ Unit unit_of(const Params& p, int L) {
         u.b = x / p.H;
         u.head[0] = u.head[1] = x - u.b * p.H;
         u.row0[0] = p.mode == 1 ? 256 * rt : 128 * rt;
-        u.row0[1] = p.mode == 1 ? u.row0[0] + 128 : 0x7fffffff;
+        u.row0[1] = p.mode == 1 ? u.row0[0] + 128 : 1 << 30;      // (behind any row, and far from where int ends)
     }
     u.hk = u.head[0] / p.group;
     u.rows = p.w.rows(u.b);
     u.keys = p.w.keys(u.b);
+    Blocks tile[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
-        u.tile[t] = u.row0[t] < u.rows ? key_blocks(p.w, u.row0[t], min(u.row0[t] + 128, u.rows), u.rows, u.keys) : Blocks{0, 0, 0};
-    u.all = u.tile[0].join(u.tile[1]);
+        tile[t] = u.row0[t] < u.rows ? key_blocks(p.w, u.row0[t], min(u.row0[t] + 128, u.rows), u.rows, u.keys) : Blocks{0, 0, 0};
+    u.all = tile[0].join(tile[1]);
     u.n = u.all.count();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        u.first[t] = tile[t].first;
+        u.from[t] = tile[t].from - u.all.from + u.all.first;
+        u.count[t] = tile[t].to - tile[t].from;
+    }
     return u;
+}
+
+// The first of a softmax warp's sixteen rows in its tile, and the tile.
+__device__ __forceinline__ int row_of_warp(int warp) { return 32 * (warp & 3) + 16 * (warp >> 3); }
+__device__ __forceinline__ int tile_of_warp(int warp) { return (warp >> 2) & 1; }
+
+// Of the warp's rows: keys from none_from on are seen by none, nor, but for the first tokens, those below none_below; those from all_from
+// up to all_to by all (so are the first tokens below all_to).  What lies between is compared.  free: the entries of the unit's list that all
+// rows see whole, from where and how many.
+__device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int warp, int4& bounds, int2& free) {
+    const int t = tile_of_warp(warp), row0 = (t ? u.row0[1] : u.row0[0]) + row_of_warp(warp), rows = u.rows, keys = u.keys;
+    int none_from = 0, none_below = 0, all_from = 0, all_to = 0;
+    if (row0 < rows) {
+        const int p0 = row0 + keys - rows, p1 = min(row0 + 16, rows) - 1 + keys - rows;
+        w.near(p0, keys, none_below, all_to);
+        w.near(p1, keys, all_from, none_from);
+        if (p0 < w.n_full && p1 >= 0) {                  // full rows among them
+            none_from = keys;
+            none_below = 0;
+            int hi;
+            w.seen(p1, keys, all_from, hi);
+            if (p0 >= 0 && p1 < w.n_full) all_to = keys;
+        }
+    }
+    bounds = make_int4(none_from, none_below, all_from, all_to);
+    const int gap = u.all.from - u.all.first, from = max((all_from + 63) >> 6, u.all.from) - gap, to = min(all_to >> 6, u.all.to) - gap;
+    free = make_int2(from, none_from > 0 && to > from ? to - from : 0);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -208,10 +256,37 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
         int L = blockIdx.x;
         for (uint32_t i = 0;; ++i) {
             if (i > 1 && !wait_lane0(bUE + 8 * (i & 1), ((i >> 1) & 1) ^ 1)) break;
-            if (lane == 0) {
-                ctl->unit[i & 1] = L;
-                mbar_arrive(bUF + 8 * (i & 1));
+            Unit& to = ctl->unit[i & 1];
+            if (L >= 0) {
+                const Unit u = unit_of(prm, L);
+                if (lane < SOFTMAX_WARPS) {
+                    int4 bounds;
+                    int2 free;
+                    bounds_of(prm.w, u, lane, bounds, free);
+                    to.bounds[lane] = bounds;
+                    to.free[lane] = free;
+                }
+                if (lane == 0) {
+                    to.n = u.n;
+                    to.b = u.b;
+                    to.hk = u.hk;
+                    to.rows = u.rows;
+                    to.keys = u.keys;
+                    to.all = u.all;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        to.head[t] = u.head[t];
+                        to.row0[t] = u.row0[t];
+                        to.first[t] = u.first[t];
+                        to.from[t] = u.from[t];
+                        to.count[t] = u.count[t];
+                    }
+                }
+            } else if (lane == 0) {
+                to.n = -1;
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bUF + 8 * (i & 1));
             if (L < 0) break;
             if (!wait_lane0(bNE, i & 1)) break;          // the unit is nearly through
             if (lane == 0) {
@@ -234,9 +309,8 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
         bool ok = true;
         for (uint32_t i = 0; ok; ++i) {
             if (!(ok = wait_lane0(bUF + 8 * (i & 1), (i >> 1) & 1))) break;
-            const int L = ctl->unit[i & 1];
-            if (L < 0) break;
-            const Unit u = unit_of(prm, L);
+            const Unit& u = ctl->unit[i & 1];
+            if (u.n < 0) break;
             if (u.n == 0 && lane == 0) mbar_arrive(bNE);
             // the last key's block, where rows behind it may hold anything
             const int tail = u.keys < prm.w.n_kv && (u.keys & 63) ? u.keys >> 6 : -1;
@@ -279,7 +353,7 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
                 if (gi == 0) {                           // the unit before has computed its last scores: its Q can go
                     if (n_q > 0 && !(ok = wait_lane0(bQE, (n_q - 1) & 1))) break;
                     if (lane == 0) {
-                        const int tiles = u.tile[1].count() > 0 ? 2 : 1;       // (a first tile without blocks is loaded all the same)
+                        const int tiles = u.tiles();       // (a first tile without blocks is loaded all the same)
                         mbar_arrive_expect_tx(bQ, tiles * C::QTILE_BYTES);
 #pragma unroll
                         for (int a = 0; a < 4; ++a)
@@ -324,11 +398,12 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
             bool ok = true;
             for (uint32_t i = 0; ok; ++i) {
                 if (!(ok = mma_wait(bUF + 8 * (i & 1), (i >> 1) & 1))) break;
-                const int L = ctl->unit[i & 1];
-                if (L < 0) break;
-                const Unit u = unit_of(prm, L);
+                const Unit& u = ctl->unit[i & 1];
                 const int n_u = u.n, n_pv0 = n_pv;
-                const Blocks mine = t ? u.tile[1] : u.tile[0];
+                if (n_u < 0) break;
+                const int use_first = u.first[t], use_from = u.from[t];
+                const uint32_t use_count = u.count[t];
+                auto used = [&](int j) { return (uint32_t)(j - use_from) < use_count || j < use_first; };
                 auto k_step = [&](int j) -> bool {       // waits for group j, then issues S = Q K(j)^T
                     const uint32_t s = (G0 + j) % KS;
                     if (!mma_wait(bKF + 8 * s, ((G0 + j) / KS) & 1)) return false;
@@ -336,7 +411,7 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
                         if (leader) mbar_arrive(bKE + 8 * s);
                         return true;
                     }
-                    if (mine.has(u.all.at(j))) {
+                    if (used(j)) {
                         tc_fence_after();
                         const uint32_t tS = tbase + 64 * (n_qk % NBUF), kb = sK + s * C::KV_BYTES;
                         if (leader) {
@@ -361,7 +436,7 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
                     // S(n + NBUF - 1) reuses the buffer of P(n - 1); the MMAs of the issuing thread execute in issue order
                     if (j + AHEAD <= n_u && !(ok = k_step(j + AHEAD))) break;
                     const uint32_t s = (W0 + j) % VS;
-                    if (mine.has(u.all.at(j))) {
+                    if (used(j)) {
                         if (!(ok = mma_wait(bPFt + 8 * (n_pv % NBUF), (n_pv / NBUF) & 1))) break;
                         tc_fence_after();
                         const uint32_t tP = tbase + 64 * (n_pv % NBUF), vb = sV + s * C::KV_BYTES;
@@ -394,9 +469,9 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
     } else {
         // ------------------------------------------------------------ softmax, epilogue
         reg_inc<SOFTMAX_REGS>();
-        const int t = (warp >> 2) & 1, wl = warp & 3, hf = warp >> 3;
+        const int t = tile_of_warp(warp);
         const int cg = lane & 3;                         // column pair within a group of eight
-        const int row_w = wl * 32 + hf * 16;             // the warp's first row of the tile
+        const int row_w = row_of_warp(warp);
         const uint32_t lane_addr = tmem_base + ((uint32_t)row_w << 16) + t * TILE_COLS, tO = lane_addr + O_COL;
         const uint32_t bSFt = bSF + 24 * t, bPFt = bPF + 24 * t, bPVt = bPV + 16 * t;
         const float c2 = prm.scale_log2;
@@ -404,60 +479,56 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
         uint32_t n_o = 0;
         for (uint32_t i = 0;; ++i) {
             if (!wait_warp(bUF + 8 * (i & 1), (i >> 1) & 1)) break;
-            const int L = ctl->unit[i & 1];
-            if (L < 0) break;
-            // what the loop needs of the unit
-            Blocks all, mine;
-            int b, head, row, rows, lo0 = 0, hi0 = 0, lo1 = 0, hi1 = 0, n_u;
-            {
-                const Unit u = unit_of(prm, L);
-                all = u.all;
-                mine = t ? u.tile[1] : u.tile[0];
-                b = u.b;
-                head = t ? u.head[1] : u.head[0];
-                rows = u.rows;
-                n_u = u.n;
-                row = (t ? u.row0[1] : u.row0[0]);
-                row = row < rows ? row + row_w + (lane >> 2) : rows;           // of a tile without rows: none
-                if (row < rows) prm.w.seen(row + u.keys - rows, u.keys, lo0, hi0);
-                if (row + 8 < rows) prm.w.seen(row + 8 + u.keys - rows, u.keys, lo1, hi1);
-            }
-            // Of the warp's rows: keys from none_from on are seen by none, those below all_to and from all_from on by all (so are the first
-            // tokens below all_to); what lies between is compared.  Rows that are not there have hi = 0 and count as seeing all.
-            const int n_sink = prm.w.n_sink;
-            const bool r0 = row < rows, r1 = row + 8 < rows;
-            const int none_from = __reduce_max_sync(0xffffffffu, max(hi0, hi1));
-            const int none_below = __reduce_min_sync(0xffffffffu, min(r0 ? lo0 : 0x7fffffff, r1 ? lo1 : 0x7fffffff));
-            const int all_from = __reduce_max_sync(0xffffffffu, max(lo0, lo1));
-            const int all_to = __reduce_min_sync(0xffffffffu, min(r0 ? hi0 : 0x7fffffff, r1 ? hi1 : 0x7fffffff));
+            const Unit& u = ctl->unit[i & 1];
+            const int n_u = u.n;
+            if (n_u < 0) break;
+            // the loop keeps no more of them, it is short of registers
+            const int free_from = u.free[warp].x;
+            const uint32_t free_count = u.free[warp].y;
             float nm_lo = LOWEST, nm_hi = LOWEST;        // reference maxima of the two rows, times -c2
             float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
             uint32_t r[32];
             const int n0 = n;
             bool seeded = false;
-            for (int j0 = 0; j0 < n_u; j0 += ABORT_EVERY) {
-                if (__any_sync(0xffffffffu, ctl->abort_flag)) break;
-                const int j1 = min(j0 + ABORT_EVERY, n_u);
-                for (int j = j0; j < j1; ++j) {
-                    const int kb = all.at(j), key0 = kb * 64;
-                    if (!mine.has(kb)) continue;
+            // One block; FREE: all of the warp's rows see it whole.  (Two copies of the code: the one that most blocks take holds nothing else.)
+            auto block = [&](int j, auto free) {
+                    constexpr bool FREE = decltype(free)::value;
+                    bool act = true, compare = false;
+                    int key0 = 0;
+                    if constexpr (!FREE) {
+                        if ((uint32_t)(j - u.from[t]) >= (uint32_t)u.count[t] && j >= u.first[t]) return;      // none of the tile's rows sees it
+                        const int4 bd = u.bounds[warp];
+                        const int n_sink = prm.w.n_sink;
+                        key0 = 64 * u.all.at(j);
+                        act = key0 < bd.x && (key0 + 64 > bd.y || key0 < n_sink);
+                        compare = key0 + 64 > bd.w || (key0 < bd.z && key0 + 64 > n_sink);
+                    }
                     const int buf = n % NBUF;
                     const uint32_t tS = lane_addr + 64 * buf;
                     wait(bSFt + 8 * buf, (n / NBUF) & 1);
                     __syncwarp();
                     tc_fence_after();
                     uint32_t pk[16];
-                    if (key0 < none_from && (key0 + 64 > none_below || key0 < n_sink)) {
+                    if (act) {
                         tmem_ld16x256_x8(tS, r);
                         tc_wait_ld();
-                        if (key0 + 64 > all_to || (key0 < all_from && key0 + 64 > n_sink)) {
+                        if (!FREE && compare) {
+                            // the keys of the block that the two rows see, as bits; the thread's columns 8 k + 2 cg + x at 8 k + x
+                            uint32_t w0[2], w1[2];
+                            const int row = u.row0[t] + row_w + (lane >> 2), rows = u.rows, keys = u.keys;
+                            prm.w.seen_bits(row + keys - rows, row < rows ? keys : 0, key0, w0);
+                            prm.w.seen_bits(row + 8 + keys - rows, row + 8 < rows ? keys : 0, key0, w1);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                w0[h] >>= 2 * cg;
+                                w1[h] >>= 2 * cg;
+                            }
 #pragma unroll
                             for (int k = 0; k < 8; ++k)
 #pragma unroll
                                 for (int x = 0; x < 2; ++x) {
-                                    const int key = key0 + 8 * k + 2 * cg + x;
-                                    if (key >= hi0 || (key < lo0 && key >= n_sink)) r[4 * k + x] = 0xff800000u;
-                                    if (key >= hi1 || (key < lo1 && key >= n_sink)) r[4 * k + 2 + x] = 0xff800000u;
+                                    if (!(w0[k >> 2] >> (8 * (k & 3) + x) & 1u)) r[4 * k + x] = 0xff800000u;
+                                    if (!(w1[k >> 2] >> (8 * (k & 3) + x) & 1u)) r[4 * k + 2 + x] = 0xff800000u;
                                 }
                         }
                         // P = 2^(S c2 - m c2) with the reference maxima as they stand; only when a partial sum of eight exceeds 2^8 the
@@ -521,45 +592,59 @@ window_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ C
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bPFt + 8 * buf);
                     ++n;
-                }
+            };
+            for (int j0 = 0; j0 < n_u;) {
+                if (__any_sync(0xffffffffu, ctl->abort_flag)) break;
+                const bool free = (uint32_t)(j0 - free_from) < free_count;
+                const int j1 = min(j0 + ABORT_EVERY, free ? free_from + (int)free_count : j0 < free_from && free_count > 0 ? free_from : n_u);
+                if (free) for (; j0 < j1; ++j0) block(j0, std::true_type());
+                else for (; j0 < j1; ++j0) block(j0, std::false_type());
             }
-            if (n > n0) wait(bOD + 8 * t, n_o++ & 1);
-            if (!__all_sync(0xffffffffu, !ctl->abort_flag)) break;
-            // epilogue: O / l, 16 bytes a lane, four lanes a 64-byte piece of a row
-            tc_fence_after();
+            // epilogue: lse and 1 / l while the last product runs; O / l, 16 bytes a lane, four lanes a 64-byte piece of a row
             float s_lo = l0 + l1, s_hi = l2 + l3;
             s_lo += __shfl_xor_sync(0xffffffffu, s_lo, 1);
             s_hi += __shfl_xor_sync(0xffffffffu, s_hi, 1);
             s_lo += __shfl_xor_sync(0xffffffffu, s_lo, 2);
             s_hi += __shfl_xor_sync(0xffffffffu, s_hi, 2);
-            const float inv_lo = s_lo > 0.f ? 1.f / s_lo : 0.f, inv_hi = s_hi > 0.f ? 1.f / s_hi : 0.f;   // a row that sees nothing: zeros
+            const float inv_lo = s_lo > 0.f ? __fdividef(1.f, s_lo) : 0.f, inv_hi = s_hi > 0.f ? __fdividef(1.f, s_hi) : 0.f;   // a row that sees nothing: zeros
+            const int b = u.b, head = u.head[t], row = u.row0[t] + row_w + (lane >> 2);
+            const bool r0 = row < u.rows, r1 = row + 8 < u.rows;
+            if (__any_sync(0xffffffffu, ctl->abort_flag)) break;
+            if (prm.lse && cg == 0) {
+                float* const to = prm.lse + ((long long)b * prm.H + head) * prm.w.n_q + row;
+                if (r0) to[0] = s_lo > 0.f ? (__log2f(s_lo) - nm_lo) * 0.69314718055994531f : -INFINITY;
+                if (r1) to[8] = s_hi > 0.f ? (__log2f(s_hi) - nm_hi) * 0.69314718055994531f : -INFINITY;
+            }
             char* const o_lo = prm.out.row(b, head, row) + 16 * cg;
             char* const o_hi = o_lo + 16 * prm.out.n;
+            if (n > n0) wait(bOD + 8 * t, n_o++ & 1);
+            if (!__all_sync(0xffffffffu, !ctl->abort_flag)) break;
+            tc_fence_after();
 #pragma unroll
-            for (int ch = 0; ch < D / 32; ++ch) {
-                uint32_t o[16];
+            for (int ch = 0; ch < D / 32; ch += 2) {
+                uint32_t o[2][16];
                 if (n > n0) {
-                    tmem_ld16x256_x4(tO + ch * 32, o);
+                    tmem_ld16x256_x4(tO + ch * 32, o[0]);
+                    tmem_ld16x256_x4(tO + ch * 32 + 32, o[1]);
                     tc_wait_ld();
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = 0u;
+                    for (int e = 0; e < 16; ++e) o[0][e] = o[1][e] = 0u;
                 }
-                uint32_t w_lo[4], w_hi[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    w_lo[k] = pack16<TYPE>(__uint_as_float(o[4 * k]) * inv_lo, __uint_as_float(o[4 * k + 1]) * inv_lo);
-                    w_hi[k] = pack16<TYPE>(__uint_as_float(o[4 * k + 2]) * inv_hi, __uint_as_float(o[4 * k + 3]) * inv_hi);
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t w_lo[4], w_hi[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        w_lo[k] = pack16<TYPE>(__uint_as_float(o[x][4 * k]) * inv_lo, __uint_as_float(o[x][4 * k + 1]) * inv_lo);
+                        w_hi[k] = pack16<TYPE>(__uint_as_float(o[x][4 * k + 2]) * inv_hi, __uint_as_float(o[x][4 * k + 3]) * inv_hi);
+                    }
+                    const uint4 v_lo = quad_transpose(w_lo[0], w_lo[1], w_lo[2], w_lo[3], cg);
+                    const uint4 v_hi = quad_transpose(w_hi[0], w_hi[1], w_hi[2], w_hi[3], cg);
+                    if (r0) *reinterpret_cast<uint4*>(o_lo + 64 * (ch + x)) = v_lo;
+                    if (r1) *reinterpret_cast<uint4*>(o_hi + 64 * (ch + x)) = v_hi;
+                    __syncwarp();
                 }
-                const uint4 v_lo = quad_transpose(w_lo[0], w_lo[1], w_lo[2], w_lo[3], cg);
-                const uint4 v_hi = quad_transpose(w_hi[0], w_hi[1], w_hi[2], w_hi[3], cg);
-                if (r0) *reinterpret_cast<uint4*>(o_lo + 64 * ch) = v_lo;
-                if (r1) *reinterpret_cast<uint4*>(o_hi + 64 * ch) = v_hi;
-            }
-            if (prm.lse && cg == 0) {
-                float* const to = prm.lse + ((long long)b * prm.H + head) * prm.w.n_q + row;
-                if (r0) to[0] = s_lo > 0.f ? (log2f(s_lo) - nm_lo) * 0.69314718055994531f : -INFINITY;
-                if (r1) to[8] = s_hi > 0.f ? (log2f(s_hi) - nm_hi) * 0.69314718055994531f : -INFINITY;
             }
             tc_fence_before();
             __syncwarp();
@@ -717,11 +802,12 @@ int rapid3_window_attn(const rapid3_window* w, const rapid3_rows* q, const rapid
     p.mode = tiles <= SM_COUNT ? 2 : p.group % 2 == 0 ? 0 : 1;
     p.heads = w->B * w->H / (p.mode == 0 ? 2 : 1);
     p.row_tiles = p.mode == 1 ? (w->n_q + 255) / 256 : (w->n_q + 127) / 128;
-    p.units = p.heads * p.row_tiles;
+    const long long full = std::min<long long>(w->n_q, w->n_full ? (long long)w->n_full + w->n_q - w->n_kv : 0);    // rows, of full sequences
+    p.full_tiles = full > 0 ? (int)((full + (p.mode == 1 ? 255 : 127)) / (p.mode == 1 ? 256 : 128)) : 0;
     const bool bf = w->type == RAPID3_BF16;
     const auto kernel = w->D == 128 ? (bf ? window_kernel<128, RAPID3_BF16> : window_kernel<128, RAPID3_F16>)
                                     : (bf ? window_kernel<64, RAPID3_BF16> : window_kernel<64, RAPID3_F16>);
-    return launch_kernel(kernel, dim3(p.units), dim3(NTHREADS), w->D == 128 ? smem_bytes<128>() : smem_bytes<64>(), st, tq, tk, tv, p) == cudaSuccess
+    return launch_kernel(kernel, dim3(p.heads * p.row_tiles), dim3(NTHREADS), w->D == 128 ? smem_bytes<128>() : smem_bytes<64>(), st, tq, tk, tv, p) == cudaSuccess
                ? RAPID3_OK : RAPID3_ERR_CUDA;
 }
 

@@ -11,6 +11,13 @@ namespace window {
 // Lengths and bounds stay below this, so that sums of two stay in 32 bits.
 constexpr int MOST = (1 << 30) - 2;
 
+// Bits 0 .. n - 1 of 32 (n of any size or sign).
+__device__ __forceinline__ uint32_t bits_below(int n) {
+    uint32_t d;
+    asm("bmsk.clamp.b32 %0, %1, %2;" : "=r"(d) : "r"(0), "r"(max(n, 0)));
+    return d;
+}
+
 struct Rule {
     int n_q, n_kv;               // places of a sequence
     int left, right;             // -1: no bound
@@ -19,11 +26,27 @@ struct Rule {
     const int32_t* kv_len;
     __device__ __forceinline__ int rows(int b) const { return q_len ? min(max(__ldcg(q_len + b), 0), n_q) : n_q; }
     __device__ __forceinline__ int keys(int b) const { return kv_len ? min(max(__ldcg(kv_len + b), 0), n_kv) : n_kv; }
-    // The row at position p sees the keys j < hi with j >= lo or j < n_sink.
+    // The row at position p sees the keys j < hi with j >= lo or j < n_sink.  near: as if no row were full.
+    __device__ __forceinline__ void near(int p, int keys, int& lo, int& hi) const {
+        lo = left < 0 ? 0 : max(p - left, 0);
+        hi = right < 0 ? keys : min(keys, max(p + right + 1, 0));
+    }
     __device__ __forceinline__ void seen(int p, int keys, int& lo, int& hi) const {
-        const bool full = (unsigned)p < (unsigned)n_full;
-        lo = full || left < 0 ? 0 : max(p - left, 0);
-        hi = full || right < 0 ? keys : min(keys, max(p + right + 1, 0));
+        near(p, keys, lo, hi);
+        if ((unsigned)p < (unsigned)n_full) {
+            lo = 0;
+            hi = keys;
+        }
+    }
+    // The same of the 64 keys from key0 on, as bits.
+    __device__ __forceinline__ void seen_bits(int p, int keys, int key0, uint32_t (&bits)[2]) const {
+        int lo, hi;
+        seen(p, keys, lo, hi);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = key0 + 32 * h;
+            bits[h] = bits_below(hi - k) & (~bits_below(lo - k) | bits_below(n_sink - k));
+        }
     }
 };
 
