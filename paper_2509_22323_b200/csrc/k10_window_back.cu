@@ -2,17 +2,22 @@
 //   P = exp(scale q k - lse) on the visible pairs, dP = dO V^T, dS = P (dP - delta), delta = sum over channels of dO O
 //   dV = P^T dO,  dK = scale dS^T Q (summed over the query heads of a key head),  dQ = scale dS K
 //
-// No number is added to by two thread blocks, so the order of the sums is fixed and the same call gives the same bits: one kernel
+// No number is added to by two thread blocks, so the order of the sums is fixed and the same call gives the same bits: a unit of work
 // keeps a tile of 128 keys (or of 128 query rows) and streams blocks of 64 query rows (or keys) past it,
-//   KEYS:   X1, X2 = K, V of the tile; Y1, Y2 = Q, dO of a block:  S^T = K Q^T, dP^T = V dO^T, then dV += P^T dO, dK += dS^T Q
-//   else:   X1, X2 = Q, dO of the tile; Y1, Y2 = K, V of a block:  S = Q K^T,   dP = dO V^T,   then dQ += dS K
+//   key unit:   X1, X2 = K, V of the tile; Y1, Y2 = Q, dO of a block:  S^T = K Q^T, dP^T = V dO^T, then dV += P^T dO, dK += dS^T Q
+//   row unit:   X1, X2 = Q, dO of the tile; Y1, Y2 = K, V of a block:  S = Q K^T,   dP = dO V^T,   then dQ += dS K
 // seven products where five are the least (the scores and dP are computed twice); the other way, dQ by atomic additions of 32-bit partial
 // sums to memory, costs 512 bytes of them for every row of every block and gives other bits on every call.
 // P and dS go back to tensor memory, rounded to the tensors' type, as the first operand of the second products.
 //
-// Roles (576 threads): warps 0-15 the element work, eight warps per score buffer (blocks go to the two buffers by turns): a warp owns 16
+// Both kinds of unit are one launch, the longest first: one thread block per SM works through them as in K8, and a unit's first loads and
+// products run beside the last one's results on their way out.  Tiles of first tokens see every row, far more than the others: where they
+// alone would keep a few SMs busy their blocks are shared out to several units, whose 32-bit results add_parts_kernel adds up.
+//
+// Roles (640 threads): warps 0-15 the element work, eight warps per score buffer (blocks go to the two buffers by turns): a warp owns 16
 // rows of the tile, a thread a quarter of two rows; warp 16 the producer (TMA; rows behind a sequence's last, which are not the caller's to
-// keep finite, are set to zero); warp 17 the UMMA issue: S and dP of block n + 1 go out before the second products of block n.
+// keep finite, are set to zero); warp 17 the UMMA issue: S and dP of block n + 1 go out before the second products of block n; warp 18 the
+// next unit.
 // TMEM: 0 and D: the accumulators; 256 + 64 (n & 1): S; 384 + 64 (n & 1): dP.
 // Every mbarrier wait is bounded, as in K8.
 #include <math.h>
@@ -20,6 +25,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "window.cuh"
 
@@ -28,19 +34,28 @@ using namespace window;
 
 namespace {
 
-constexpr int WARPS = 16, PRODUCER_WARP = 16, MMA_WARP = 17, NTHREADS = 32 * (WARPS + 2);
+constexpr int WARPS = 16, PRODUCER_WARP = 16, MMA_WARP = 17, NEXT_WARP = 18, NTHREADS = 32 * (WARPS + 4);
+constexpr int ELEMENT_REGS = 104, LIGHT_REGS = 64;       // registers a thread of the element warps, of the others: of 640 x 96
 constexpr int TMEM_COLS = 512, S_COL = 256, DP_COL = 384;
 constexpr int BLK_BYTES = 8192, XHALF_BYTES = 16384;
+constexpr int TAKE_AHEAD = 4, UNIT_USERS = WARPS + 2;
+constexpr int MAX_PARTS = 16, MAX_SLOTS = 2 * SM_COUNT;  // units of a shared-out tile; of all of them
 
 __device__ int status_word;
 
 struct Params {
     Rule w;
-    Rows g1, g2;                 // KEYS: dK, dV; else dQ
-    const float* lse2;           // [B][H][padded]: log sum exp in base 2; +inf: a row that has no P
-    const float* delta;
+    Rows dq, dk, dv;
+    const float* nlse;           // [B][H][padded]: minus log sum exp in base 2; -inf: a row that has no P
+    const float* ndelta;         // minus delta
+    float* partial;              // [slot][128][2 D]
     int padded;                  // query rows of a head in these, a multiple of 64
-    int H, H_kv, group, tiles;   // tiles of a head
+    int H, H_kv, group;
+    int key_tiles, row_tiles;    // of a head
+    int sink_tiles, parts;       // the first key tiles, and how many units share one
+    int full_tiles;              // the first row tiles
+    int sink_units, key_units, full_units;   // where the kinds end in the order of the units: sink tiles, other key tiles, full row tiles, other row tiles
+    bool last_first;             // the last rows have the most keys
     float scale, scale_log2;
 };
 
@@ -48,45 +63,163 @@ template <int D>
 struct Cfg {
     static constexpr int DH = D / 64;
     static constexpr int XTILE_BYTES = 128 * D * 2, Y_BYTES = 64 * D * 2;
-    static constexpr int STAT_BYTES = 512;                              // KEYS: lse2 and delta of the block's 64 rows
+    static constexpr int STAT_BYTES = 512;               // key unit: nlse and ndelta of the block's 64 rows
     static constexpr int STAGES = D == 128 ? 4 : 6;
     static constexpr int STAGE_BYTES = 2 * Y_BYTES;
     static constexpr int DATA_BYTES = 2 * XTILE_BYTES + STAGES * (STAGE_BYTES + STAT_BYTES);
 };
 constexpr int MAX_STAGES = 6;
 
+// A unit of work, written by the warp that takes it over.
+struct Unit {
+    int n;                       // its blocks, of all heads; -1: no more units
+    int key;                     // a key unit
+    int b, h, first, end;        // sequence, head (a key unit's: key head), first row of the tile, rows (keys) of the sequence
+    int rows, keys;
+    Blocks blocks;               // of one head
+    int per_head, begin;         // a head's blocks; the first block of this part, through all heads
+    int slot;                    // of a shared-out tile: where its result goes, else -1
+    // Of an element warp's rows (eight groups of sixteen): columns in [x, y) and in [z, w) are seen by all rows; reach: by some at most from x up to y and
+    // below z.
+    int4 whole[8];
+    int3 reach[8];
+};
+
 struct __align__(16) Ctl {
-    unsigned long long x_full, tail_full, full[MAX_STAGES], empty[MAX_STAGES], t_full[2], p_full[2], done, drain;
+    uint4 taken;
+    unsigned long long taken_full, near_end, unit_full[2], unit_empty[2];
+    unsigned long long x_full, x_empty, tail_full, full[MAX_STAGES], empty[MAX_STAGES], t_full[2], p_full[2], done, drained, drain;
     uint32_t tmem_base;
     volatile int abort_flag;
+    Unit unit[2];
 };
 template <int D>
 constexpr size_t smem_bytes() { return (size_t)Cfg<D>::DATA_BYTES + sizeof(Ctl) + 1024; }
 
-// The blocks of 64 query rows that see any of the keys [k0, k1).
+// Of a key: it is seen by the rows [lo, hi), and by the full ones.
+__device__ __forceinline__ void rows_of_key(const Rule& w, int key, int rows, int off, int& lo, int& hi) {
+    lo = w.right < 0 ? 0 : min(max(key - w.right - off, 0), rows);
+    hi = w.left < 0 || key < w.n_sink ? rows : min(max(key + w.left + 1 - off, 0), rows);
+}
+// The full rows [lo, hi).
+__device__ __forceinline__ void full_rows(const Rule& w, int rows, int off, int& lo, int& hi) {
+    lo = min(max(-off, 0), rows);
+    hi = w.n_full == 0 ? lo : min(max(w.n_full - off, lo), rows);
+}
+// The blocks of 64 query rows that see any of the keys [k0, k1), k1 <= keys.
 __device__ __forceinline__ Blocks query_blocks(const Rule& w, int k0, int k1, int rows, int keys) {
-    if (k0 >= keys) return {0, 0, 0};
-    k1 = min(k1, keys);
-    const int off = keys - rows;
-    const int full = w.n_full == 0 ? 0 : min(max(w.n_full - off, 0), rows);   // behind the rows that see every key (before them there may be rows without a position)
-    const int from = w.right < 0 ? 0 : min(max(k0 - w.right - off, 0), rows);
-    const int to = w.left < 0 || k0 < w.n_sink ? rows : min(max(k1 + w.left - off, 0), rows);
+    if (k0 >= k1) return {0, 0, 0};
+    int from, to, x, full;
+    rows_of_key(w, k0, rows, keys - rows, from, to);
+    if (k0 >= w.n_sink) rows_of_key(w, k1 - 1, rows, keys - rows, x, to);
+    full_rows(w, rows, keys - rows, x, full);
+    if (full <= x) full = 0;
+    const int full_blocks = (full + 63) >> 6;
     Blocks r;
     if (to <= from) {
-        r.from = r.to = r.first = (full + 63) >> 6;
+        r.from = r.to = r.first = full_blocks;
         return r;
     }
     r.from = from >> 6;
-    r.to = (to + 63) >> 6;
-    r.first = min((full + 63) >> 6, r.from);
-    if (((full + 63) >> 6) > r.to) r.to = (full + 63) >> 6;             // (the window's rows lie among the full ones)
+    r.to = max((to + 63) >> 6, full_blocks);
+    r.first = min(full_blocks, r.from);
     return r;
 }
 
-template <int D, int TYPE, bool KEYS>
+// Of sixteen rows of a tile, see Unit::whole and reach.
+__device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int group, int4& whole, int3& reach) {
+    const int r0 = u.first + 16 * group, r1 = min(r0 + 16, u.end) - 1, off = u.keys - u.rows;
+    whole = make_int4(0, 0, 0, 0);
+    reach = make_int3(0, 0, 0);
+    if (r0 > r1) return;
+    if (u.key) {
+        int lo, hi, from, to;
+        rows_of_key(w, r0, u.rows, off, from, hi);       // from: the least; hi: the least unless the row is a first token
+        rows_of_key(w, r1, u.rows, off, lo, to);
+        if (r0 < w.n_sink) {
+            to = u.rows;
+            int x;
+            if (r1 >= w.n_sink) rows_of_key(w, w.n_sink, u.rows, off, x, hi);
+        }
+        int full_lo, full_hi;
+        full_rows(w, u.rows, off, full_lo, full_hi);
+        whole = make_int4(lo, hi, full_lo, full_hi);
+        reach = make_int3(from, to, full_hi);
+    } else {
+        const int p0 = r0 + off, p1 = r1 + off;
+        int lo, hi, from, to;
+        w.near(p0, u.keys, from, hi);
+        w.near(p1, u.keys, lo, to);
+        if (p0 < w.n_full && p1 >= 0) {                  // full rows among them
+            int x;
+            from = 0;
+            to = u.keys;
+            w.seen(p1, u.keys, lo, x);
+            if (p0 >= 0 && p1 < w.n_full) hi = u.keys;
+        }
+        whole = make_int4(lo, hi, 0, min(w.n_sink, hi));
+        reach = make_int3(from, to, min(w.n_sink, to));
+    }
+}
+
+__device__ __forceinline__ Unit unit_of(const Params& p, int B, int L) {
+    Unit u;
+    u.key = L < p.key_units;
+    u.slot = -1;
+    const int heads = B * (u.key ? p.H_kv : p.H);
+    int part = 0, parts = 1, x, tile;
+    if (L < p.sink_units) {
+        parts = p.parts;
+        x = L / parts;
+        part = L - x * parts;
+        if (parts > 1) u.slot = L;
+        tile = x / heads;                                // tiles of first tokens: of all heads side by side
+        x -= tile * heads;
+    } else {
+        const bool full = !u.key && L < p.full_units;
+        const int tiles = u.key ? p.key_tiles - p.sink_tiles : full ? p.full_tiles : p.row_tiles - p.full_tiles;
+        const int y = L - (u.key ? p.sink_units : full ? p.key_units : p.full_units);
+        x = y / tiles;                                   // head by head, whose units share what they stream in the L2
+        tile = y - x * tiles;
+        if (!u.key && p.last_first) tile = tiles - 1 - tile;
+        tile += u.key ? p.sink_tiles : full ? 0 : p.full_tiles;
+    }
+    const int per = u.key ? p.H_kv : p.H;
+    u.b = x / per;
+    u.h = x - u.b * per;
+    u.rows = p.w.rows(u.b);
+    u.keys = p.w.keys(u.b);
+    u.first = 128 * tile;
+    u.end = u.key ? u.keys : u.rows;
+    const int last = min(u.first + 128, u.end);
+    u.blocks = u.first >= last ? Blocks{0, 0, 0} : u.key ? query_blocks(p.w, u.first, last, u.rows, u.keys)
+                                                         : key_blocks(p.w, u.first, last, u.rows, u.keys);
+    u.per_head = u.blocks.count();
+    const int n = u.key ? p.group * u.per_head : u.per_head;
+    u.begin = (int)((long long)n * part / parts);
+    u.n = (int)((long long)n * (part + 1) / parts) - u.begin;
+    return u;
+}
+
+// The blocks of a unit one after the other: of which head of the group, and which.
+struct Walk {
+    int head, j;
+    __device__ __forceinline__ Walk(const Unit& u) {
+        head = u.per_head > 0 ? u.begin / u.per_head : 0;
+        j = u.begin - head * u.per_head;
+    }
+    __device__ __forceinline__ void next(int per_head) {
+        if (++j == per_head) {
+            j = 0;
+            ++head;
+        }
+    }
+};
+
+template <int D, int TYPE>
 __global__ void __launch_bounds__(NTHREADS, 1)
-window_back_kernel(const __grid_constant__ CUtensorMap tx1, const __grid_constant__ CUtensorMap tx2, const __grid_constant__ CUtensorMap ty1,
-                   const __grid_constant__ CUtensorMap ty2, const __grid_constant__ Params prm) {
+window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+                   const __grid_constant__ CUtensorMap td, const __grid_constant__ Params prm, int B) {
     using C = Cfg<D>;
     constexpr int DH = C::DH, STAGES = C::STAGES;
     extern __shared__ uint8_t smem_raw[];
@@ -97,20 +230,25 @@ window_back_kernel(const __grid_constant__ CUtensorMap tx1, const __grid_constan
     Ctl* ctl = reinterpret_cast<Ctl*>(smem + C::DATA_BYTES);
     const int tid = threadIdx.x, lane = tid % 32;
     const int warp = __shfl_sync(0xffffffffu, tid / 32, 0);
-    const uint32_t bX = smem_u32(&ctl->x_full), bTail = smem_u32(&ctl->tail_full), bF = smem_u32(&ctl->full[0]), bE = smem_u32(&ctl->empty[0]);
-    const uint32_t bT = smem_u32(&ctl->t_full[0]), bP = smem_u32(&ctl->p_full[0]), bD = smem_u32(&ctl->done);
+    const uint32_t bX = smem_u32(&ctl->x_full), bXE = smem_u32(&ctl->x_empty), bTail = smem_u32(&ctl->tail_full);
+    const uint32_t bF = smem_u32(&ctl->full[0]), bE = smem_u32(&ctl->empty[0]), bT = smem_u32(&ctl->t_full[0]), bP = smem_u32(&ctl->p_full[0]);
+    const uint32_t bD = smem_u32(&ctl->done), bDE = smem_u32(&ctl->drained);
+    const uint32_t bUF = smem_u32(&ctl->unit_full[0]), bUE = smem_u32(&ctl->unit_empty[0]), bNE = smem_u32(&ctl->near_end), bTk = smem_u32(&ctl->taken_full);
 
     if (warp == 0) {
-        constexpr uint32_t bars = offsetof(Ctl, tmem_base) / 8;
+        constexpr uint32_t at = offsetof(Ctl, taken_full) / 8, bars = offsetof(Ctl, tmem_base) / 8 - at;
+        auto has = [&](uint32_t x, size_t member, int n) { return x + at - (uint32_t)(member / 8) < (uint32_t)n; };
         for (uint32_t x = lane; x < bars; x += 32) {
             uint32_t count = 1;
-            if (x - (uint32_t)(offsetof(Ctl, p_full) / 8) < 2u) count = 8;             // one arrival per warp of the buffer
-            mbar_init(smem_u32(ctl) + 8 * x, count);
+            if (has(x, offsetof(Ctl, unit_empty), 2)) count = UNIT_USERS;
+            if (has(x, offsetof(Ctl, p_full), 2)) count = 8;                   // one arrival per warp of the buffer
+            if (has(x, offsetof(Ctl, drained), 1)) count = WARPS;
+            mbar_init(smem_u32(ctl) + 8 * (at + x), count);
         }
         if (lane == 0) ctl->abort_flag = 0;
         fence_mbar_init();
     }
-    if (warp == PRODUCER_WARP && lane < 4) prefetch_tmap(lane == 0 ? &tx1 : lane == 1 ? &tx2 : lane == 2 ? &ty1 : &ty2);
+    if (warp == PRODUCER_WARP && lane < 4) prefetch_tmap(lane == 0 ? &tq : lane == 1 ? &tk : lane == 2 ? &tv : &td);
     if (warp == MMA_WARP) {
         tmem_alloc(smem_u32(&ctl->tmem_base), TMEM_COLS);
         tmem_relinquish();
@@ -120,16 +258,6 @@ window_back_kernel(const __grid_constant__ CUtensorMap tx1, const __grid_constan
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
-
-    // the tile: the longest ones first where the first rows or keys have the most work
-    const int heads = KEYS ? prm.H_kv : prm.H;
-    const int all_heads = gridDim.x / prm.tiles, tile = blockIdx.x / all_heads, at_head = blockIdx.x - tile * all_heads;
-    const int b = at_head / heads, h = at_head - b * heads;
-    const int rows = prm.w.rows(b), keys = prm.w.keys(b), off = keys - rows;
-    const int first = 128 * tile, end = KEYS ? keys : rows;            // first row of the tile, of so many
-    const Blocks blocks = first >= end ? Blocks{0, 0, 0} : KEYS ? query_blocks(prm.w, first, first + 128, rows, keys)
-                                                                : key_blocks(prm.w, first, min(first + 128, rows), rows, keys);
-    const int per_head = blocks.count(), n_items = KEYS ? prm.group * per_head : per_head;
 
     auto fail = [&]() {
         atomicExch(&status_word, RAPID3_ERR_TIMEOUT);
@@ -147,198 +275,327 @@ window_back_kernel(const __grid_constant__ CUtensorMap tx1, const __grid_constan
         return __shfl_sync(0xffffffffu, (int)(lane != 0 || wait(bar, parity)), 0);
     };
 
-    if (warp == PRODUCER_WARP) {
-        int n = 0;
-        uint32_t n_tail = 0;
-        if (n_items > 0) {
-            const int y_len = KEYS ? rows : keys, y_places = KEYS ? prm.w.n_q : prm.w.n_kv;
-            const int tail = y_len < y_places && (y_len & 63) ? y_len >> 6 : -1;
+    if (warp >= WARPS) reg_dec<LIGHT_REGS>();
+    if (warp == NEXT_WARP) {
+        int L = blockIdx.x;
+        for (uint32_t i = 0;; ++i) {
+            if (i > 1 && !wait_lane0(bUE + 8 * (i & 1), ((i >> 1) & 1) ^ 1)) break;
+            Unit& to = ctl->unit[i & 1];
+            if (L >= 0) {
+                const Unit u = unit_of(prm, B, L);
+                if (lane < 8) {
+                    int4 whole;
+                    int3 reach;
+                    bounds_of(prm.w, u, lane, whole, reach);
+                    to.whole[lane] = whole;
+                    to.reach[lane] = reach;
+                }
+                if (lane == 0) {
+                    to.n = u.n; to.key = u.key; to.b = u.b; to.h = u.h;
+                    to.first = u.first; to.end = u.end; to.rows = u.rows; to.keys = u.keys;
+                    to.blocks = u.blocks; to.per_head = u.per_head; to.begin = u.begin; to.slot = u.slot;
+                }
+            } else if (lane == 0) {
+                to.n = -1;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bUF + 8 * (i & 1));
+            if (L < 0) break;
+            if (!wait_lane0(bNE, i & 1)) break;          // the unit is nearly through
             if (lane == 0) {
-                mbar_arrive_expect_tx(bX, 2 * C::XTILE_BYTES);
+                mbar_arrive_expect_tx(bTk, 16);
+                clc_try_cancel(smem_u32(&ctl->taken), bTk);
+            }
+            __syncwarp();
+            // no way out before the answer is here: it is written into this thread block's shared memory
+            if (!__all_sync(0xffffffffu, mbar_wait(bTk, i & 1))) {
+                if (lane == 0) fail();
+                break;
+            }
+            L = clc_taken(smem_u32(&ctl->taken));
+        }
+    } else if (warp == PRODUCER_WARP) {
+        uint32_t N = 0, n_x = 0, n_tail = 0;             // blocks, tiles and mended blocks so far, in all units
+        bool ok = true;
+        for (uint32_t i = 0; ok; ++i) {
+            if (!(ok = wait_lane0(bUF + 8 * (i & 1), (i >> 1) & 1))) break;
+            const Unit& u = ctl->unit[i & 1];
+            const int n = u.n, per_head = u.per_head, b = u.b, h = u.h;
+            if (n < 0) break;
+            const bool key = u.key;
+            const Blocks blocks = u.blocks;
+            const CUtensorMap* const x1 = key ? &tk : &tq, * const x2 = key ? &tv : &td, * const y1 = key ? &tq : &tk, * const y2 = key ? &td : &tv;
+            const int y_len = key ? u.rows : u.keys, y_places = key ? prm.w.n_q : prm.w.n_kv;
+            const int tail = y_len < y_places && (y_len & 63) ? y_len >> 6 : -1;
+            if (n == 0 && lane == 0) mbar_arrive(bNE);
+            Walk at(u);
+            for (int j = 0; j < n; ++j, ++N, at.next(per_head)) {
+                if (j == max(n - TAKE_AHEAD, 0) && lane == 0) mbar_arrive(bNE);
+                if (j == 0) {                            // the unit before has computed its last scores: its tile can go
+                    if (n_x > 0 && !(ok = wait_lane0(bXE, (n_x - 1) & 1))) break;
+                    if (lane == 0) {
+                        const int first = u.first;
+                        mbar_arrive_expect_tx(bX, 2 * C::XTILE_BYTES);
 #pragma unroll
-                for (int a = 0; a < 2; ++a)
+                        for (int a = 0; a < 2; ++a)
+#pragma unroll
+                            for (int dh = 0; dh < DH; ++dh) {
+                                tma_load_4d(sX + dh * XHALF_BYTES + a * BLK_BYTES, x1, bX, dh * 64, first + 64 * a, h, b);
+                                tma_load_4d(sX + C::XTILE_BYTES + dh * XHALF_BYTES + a * BLK_BYTES, x2, bX, dh * 64, first + 64 * a, h, b);
+                            }
+                    }
+                    ++n_x;
+                }
+                const uint32_t s = N % STAGES;
+                const int block = blocks.at(at.j), yh = key ? h * prm.group + at.head : h / prm.group;
+                if (!(ok = wait_lane0(bE + 8 * s, ((N / STAGES) & 1) ^ 1))) break;
+                const uint32_t y = sY + s * C::STAGE_BYTES;
+                const bool mend = block == tail;
+                if (lane == 0) {
+                    const uint32_t bar = mend ? bTail : bF + 8 * s;
+                    mbar_arrive_expect_tx(bar, C::STAGE_BYTES + (key ? C::STAT_BYTES : 0));
 #pragma unroll
                     for (int dh = 0; dh < DH; ++dh) {
-                        tma_load_4d(sX + dh * XHALF_BYTES + a * BLK_BYTES, &tx1, bX, dh * 64, first + 64 * a, h, b);
-                        tma_load_4d(sX + C::XTILE_BYTES + dh * XHALF_BYTES + a * BLK_BYTES, &tx2, bX, dh * 64, first + 64 * a, h, b);
+                        tma_load_4d(y + dh * BLK_BYTES, y1, bar, dh * 64, block * 64, yh, b);
+                        tma_load_4d(y + C::Y_BYTES + dh * BLK_BYTES, y2, bar, dh * 64, block * 64, yh, b);
                     }
-            }
-            bool ok = true;
-            for (int gh = 0; ok && gh < (KEYS ? prm.group : 1); ++gh)
-                for (int j = 0; j < per_head; ++j, ++n) {
-                    const int s = n % STAGES, block = blocks.at(j), yh = KEYS ? h * prm.group + gh : h / prm.group;
-                    if (!(ok = wait_lane0(bE + 8 * s, ((n / STAGES) & 1) ^ 1))) break;
-                    const uint32_t y = sY + s * C::STAGE_BYTES;
-                    const bool mend = block == tail;
-                    if (lane == 0) {
-                        const uint32_t bar = mend ? bTail : bF + 8 * s;
-                        mbar_arrive_expect_tx(bar, C::STAGE_BYTES + (KEYS ? C::STAT_BYTES : 0));
-#pragma unroll
-                        for (int dh = 0; dh < DH; ++dh) {
-                            tma_load_4d(y + dh * BLK_BYTES, &ty1, bar, dh * 64, block * 64, yh, b);
-                            tma_load_4d(y + C::Y_BYTES + dh * BLK_BYTES, &ty2, bar, dh * 64, block * 64, yh, b);
-                        }
-                        if (KEYS) {
-                            const long long at = ((long long)b * prm.H + yh) * prm.padded + block * 64;
-                            const uint32_t to = smem_u32(stats) + s * C::STAT_BYTES;
-                            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
-                                         ::"r"(to), "l"(prm.lse2 + at), "r"(bar) : "memory");
-                            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
-                                         ::"r"(to + 256), "l"(prm.delta + at), "r"(bar) : "memory");
-                        }
-                    }
-                    __syncwarp();
-                    if (mend) {
-                        if (!(ok = wait_lane0(bTail, n_tail++ & 1))) break;
-                        uint8_t* to = smem + (y - sX);
-                        for (int z = (y_len & 63) * 8 + lane; z < 64 * 8; z += 32)
-#pragma unroll
-                            for (int dh = 0; dh < 2 * DH; ++dh) *reinterpret_cast<uint4*>(to + dh * BLK_BYTES + 16 * z) = make_uint4(0, 0, 0, 0);
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(bF + 8 * s);
+                    if (key) {
+                        const long long from = ((long long)b * prm.H + yh) * prm.padded + block * 64;
+                        const uint32_t to = smem_u32(stats) + s * C::STAT_BYTES;
+                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
+                                     ::"r"(to), "l"(prm.nlse + from), "r"(bar) : "memory");
+                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
+                                     ::"r"(to + 256), "l"(prm.ndelta + from), "r"(bar) : "memory");
                     }
                 }
-            if (ctl->abort_flag && lane == 0) {          // no copy may land after the thread block has left
-                mbar_wait(bX, 0, 1u << 20);
-                if (n_tail > 0) mbar_wait(bTail, (n_tail - 1) & 1, 1u << 20);
-                for (int z = max(0, n - STAGES); z < n; ++z) mbar_wait(bF + 8 * (z % STAGES), (z / STAGES) & 1, 1u << 20);
+                __syncwarp();
+                if (mend) {
+                    if (!(ok = wait_lane0(bTail, n_tail++ & 1))) break;
+                    uint8_t* to = smem + (y - sX);       // a row of a half is 128 bytes; the swizzle moves bytes within it
+                    for (int z = (y_len & 63) * 8 + lane; z < 64 * 8; z += 32)
+#pragma unroll
+                        for (int dh = 0; dh < 2 * DH; ++dh) *reinterpret_cast<uint4*>(to + dh * BLK_BYTES + 16 * z) = make_uint4(0, 0, 0, 0);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bF + 8 * s);
+                }
             }
+            if (!ok) break;
+            if (lane == 0) mbar_arrive(bUE + 8 * (i & 1));
+        }
+        if (ctl->abort_flag && lane == 0) {              // no copy may land after the thread block has left
+            if (n_x > 0) mbar_wait(bX, (n_x - 1) & 1, 1u << 20);
+            if (n_tail > 0) mbar_wait(bTail, (n_tail - 1) & 1, 1u << 20);
+            for (uint32_t z = N > STAGES ? N - STAGES : 0; z < N; ++z) mbar_wait(bF + 8 * (z % STAGES), (z / STAGES) & 1, 1u << 20);
         }
         __syncwarp();
     } else if (warp == MMA_WARP) {
-        if (elect_one() && n_items > 0) {
+        if (elect_one()) {
             constexpr uint32_t idesc1 = idesc16<TYPE>(128, 64, 0, 0), idesc2 = idesc16<TYPE>(128, D, 0, 1);
-            bool ok = wait(bX, 0);
-            auto first_products = [&](int n) -> bool {
-                const int s = n % STAGES;
-                if (!wait(bF + 8 * s, (n / STAGES) & 1)) return false;
-                tc_fence_after();
-                const uint32_t y = sY + s * C::STAGE_BYTES;
+            uint32_t N = 0, n_x = 0;
+            bool ok = true;
+            for (uint32_t i = 0; ok; ++i) {
+                if (!(ok = wait(bUF + 8 * (i & 1), (i >> 1) & 1))) break;
+                const int n = ctl->unit[i & 1].n;
+                const bool key = ctl->unit[i & 1].key;
+                if (n < 0) break;
+                auto first_products = [&](int j) -> bool {
+                    const uint32_t M = N + j, s = M % STAGES;
+                    if (!wait(bF + 8 * s, (M / STAGES) & 1)) return false;
+                    tc_fence_after();
+                    const uint32_t y = sY + s * C::STAGE_BYTES;
 #pragma unroll
-                for (int w = 0; w < 2; ++w)
+                    for (int w = 0; w < 2; ++w)
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
-                        mma_ss(tmem_base + (w ? DP_COL : S_COL) + 64 * (n & 1),
-                               smem_desc_sw128(sX + w * C::XTILE_BYTES + (ks / 4) * XHALF_BYTES + (ks % 4) * 32, 16, 1024),
-                               smem_desc_sw128(y + w * C::Y_BYTES + (ks / 4) * BLK_BYTES + (ks % 4) * 32, 16, 1024), idesc1, ks > 0);
-                tc_commit(bT + 8 * (n & 1));
-                return true;
-            };
-            if (ok) ok = first_products(0);
-            for (int n = 0; ok && n < n_items; ++n) {
-                // S and dP of block n + 1 take the buffers of block n - 1, whose second products were issued before
-                if (n + 1 < n_items && !(ok = first_products(n + 1))) break;
-                if (!(ok = wait(bP + 8 * (n & 1), (n >> 1) & 1))) break;
-                tc_fence_after();
-                const int s = n % STAGES;
-                const uint32_t y = sY + s * C::STAGE_BYTES;
-                // KEYS: dK += dS^T Q, dV += P^T dO; else dQ += dS K
+                        for (int ks = 0; ks < D / 16; ++ks)
+                            mma_ss(tmem_base + (w ? DP_COL : S_COL) + 64 * (M & 1),
+                                   smem_desc_sw128(sX + w * C::XTILE_BYTES + (ks / 4) * XHALF_BYTES + (ks % 4) * 32, 16, 1024),
+                                   smem_desc_sw128(y + w * C::Y_BYTES + (ks / 4) * BLK_BYTES + (ks % 4) * 32, 16, 1024), idesc1, ks > 0);
+                    tc_commit(bT + 8 * (M & 1));
+                    if (j == n - 1) tc_commit(bXE);
+                    return true;
+                };
+                if (n > 0) ok = wait(bX, n_x & 1) && first_products(0);
+                for (int j = 0; ok && j < n; ++j) {
+                    // S and dP of block j + 1 take the buffers of block j - 1, whose second products were issued before
+                    if (j + 1 < n && !(ok = first_products(j + 1))) break;
+                    const uint32_t M = N + j, s = M % STAGES;
+                    if (!(ok = wait(bP + 8 * (M & 1), (M >> 1) & 1))) break;
+                    // the first of a unit's second products overwrite the accumulators: those of the unit before have been read
+                    if (j == 0 && n_x > 0 && !(ok = wait(bDE, (n_x - 1) & 1))) break;
+                    tc_fence_after();
+                    const uint32_t y = sY + s * C::STAGE_BYTES;
+                    // key unit: dK += dS^T Q, dV += P^T dO; row unit: dQ += dS K
 #pragma unroll
-                for (int w = 0; w < (KEYS ? 2 : 1); ++w)
+                    for (int w = 0; w < 2; ++w)
+                        if (w == 0 || key)
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)
-                        mma_ts(tmem_base + w * D, tmem_base + (w ? S_COL : DP_COL) + 64 * (n & 1) + ks * 8,
-                               smem_desc_sw128(y + w * C::Y_BYTES + ks * 2048, BLK_BYTES, 1024), idesc2, (n > 0 || ks > 0) ? 1u : 0u);
-                tc_commit(bE + 8 * s);
+                            for (int ks = 0; ks < 4; ++ks)
+                                mma_ts(tmem_base + w * D, tmem_base + (w ? S_COL : DP_COL) + 64 * (M & 1) + ks * 8,
+                                       smem_desc_sw128(y + w * C::Y_BYTES + ks * 2048, BLK_BYTES, 1024), idesc2, (j > 0 || ks > 0) ? 1u : 0u);
+                    tc_commit(bE + 8 * s);
+                }
+                if (!ok) break;
+                if (n > 0) {
+                    tc_commit(bD);
+                    ++n_x;
+                }
+                N += n;
+                mbar_arrive(bUE + 8 * (i & 1));
             }
-            if (ok) tc_commit(bD);
         }
         __syncwarp();
-    } else {
-        const int set = warp >> 3, cg = lane & 3, row_w = 32 * (warp & 3) + 16 * ((warp >> 2) & 1);
-        const uint32_t lane_addr = tmem_base + ((uint32_t)row_w << 16);
-        const int row = first + row_w + (lane >> 2);     // and row + 8
+    } else if (warp < WARPS) {
+        reg_inc<ELEMENT_REGS>();
+        const int set = warp >> 3, group = 2 * (warp & 3) + ((warp >> 2) & 1), cg = lane & 3;
+        const uint32_t lane_addr = tmem_base + ((uint32_t)(16 * group) << 16);
+        const uint32_t tS = lane_addr + S_COL + 64 * set, tP = lane_addr + DP_COL + 64 * set;
         const float c2 = prm.scale_log2;
-        // Where a row of the tile and a column of a block see one another: column in [lo, hi), or below `extra` (KEYS: the full rows;
-        // else the first keys, below hi too).
-        int lo[2], hi[2], extra = KEYS ? (prm.w.n_full == 0 ? 0 : prm.w.n_full - off) : prm.w.n_sink;
-        float nl[2] = {0.f, 0.f}, dl[2] = {0.f, 0.f};
+        uint32_t N = 0, n_x = 0;
+        for (uint32_t i = 0;; ++i) {
+            if (!__all_sync(0xffffffffu, wait(bUF + 8 * (i & 1), (i >> 1) & 1))) break;
+            const Unit& u = ctl->unit[i & 1];
+            const int n = u.n;
+            if (n < 0) break;
+            // a unit's blocks, those of this warp's buffer
+            auto element_work = [&](auto is_key) {
+                constexpr bool KEY = decltype(is_key)::value;
+                float nl[2] = {0.f, 0.f}, nd[2] = {0.f, 0.f};
+                if (!KEY) {
+                    const int row = u.first + 16 * group + (lane >> 2);
+                    const long long at = ((long long)u.b * prm.H + u.h) * prm.padded + row;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = row + 8 * e;
-            lo[e] = hi[e] = 0;
-            if (r >= end) continue;
-            if (KEYS) {
-                lo[e] = prm.w.right < 0 ? 0 : max(r - prm.w.right - off, 0);
-                hi[e] = prm.w.left < 0 || r < prm.w.n_sink ? rows : min(max(r + prm.w.left + 1 - off, 0), rows);
-            } else {
-                prm.w.seen(r + off, keys, lo[e], hi[e]);
-                const long long at = ((long long)b * prm.H + h) * prm.padded + r;
-                nl[e] = -__ldcg(prm.lse2 + at);
-                dl[e] = __ldcg(prm.delta + at);
-            }
-        }
-        // columns that all of the warp's rows see for certain: [all_from, all_to)
-        const bool r0 = row < end, r1 = row + 8 < end;
-        const int all_from = __reduce_max_sync(0xffffffffu, max(lo[0], lo[1]));
-        const int all_to = __reduce_min_sync(0xffffffffu, min(r0 ? hi[0] : 0x7fffffff, r1 ? hi[1] : 0x7fffffff));
-        for (int n = set; n < n_items; n += 2) {
-            const int block = blocks.at(KEYS ? n % per_head : n), col0 = 64 * block;
-            wait(bT + 8 * set, (n >> 1) & 1);
-            if (KEYS) wait(bF + 8 * (n % STAGES), (n / STAGES) & 1);           // lse2 and delta of the block, read below
-            if (__any_sync(0xffffffffu, ctl->abort_flag)) break;
-            tc_fence_after();
-            uint32_t s[32], d[32];
-            tmem_ld16x256_x8(lane_addr + S_COL + 64 * set, s);
-            tmem_ld16x256_x8(lane_addr + DP_COL + 64 * set, d);
-            tc_wait_ld();
-            const bool compare = col0 + 64 > all_to || col0 < all_from;
-            const float* st = reinterpret_cast<const float*>(stats + (n % STAGES) * C::STAT_BYTES) + 2 * cg;
-            uint32_t pp[16], pd[16];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                float nc[2] = {0.f, 0.f}, dc[2] = {0.f, 0.f};
-                if (KEYS) {
-                    const float2 a = *reinterpret_cast<const float2*>(st + 8 * k), bb = *reinterpret_cast<const float2*>(st + 64 + 8 * k);
-                    nc[0] = -a.x; nc[1] = -a.y; dc[0] = bb.x; dc[1] = bb.y;
+                    for (int e = 0; e < 2; ++e)
+                        if (row + 8 * e < u.end) {
+                            nl[e] = __ldcg(prm.nlse + at + 8 * e);
+                            nd[e] = __ldcg(prm.ndelta + at + 8 * e);
+                        }
                 }
-                float p[4], ds[4];
+                Walk at(u);
+                const int per_head = u.per_head;
+                for (int j = 0; j < n; ++j, at.next(per_head)) {
+                    const uint32_t M = N + j;
+                    if ((int)(M & 1) != set) continue;
+                    const int col0 = 64 * u.blocks.at(at.j);
+                    const int4 whole = u.whole[group];
+                    const int3 reach = u.reach[group];
+                    const bool act = (col0 < reach.y && col0 + 64 > reach.x) || col0 < reach.z;
+                    const bool compare = !((col0 >= whole.x && col0 + 64 <= whole.y) || (col0 >= whole.z && col0 + 64 <= whole.w));
+                    wait(bT + 8 * set, (M >> 1) & 1);
+                    if (KEY) wait(bF + 8 * (M % STAGES), (M / STAGES) & 1);    // nlse and ndelta of the block, read below
+                    if (__any_sync(0xffffffffu, ctl->abort_flag)) return;
+                    tc_fence_after();
+                    if (act) {
+                        uint32_t s[2][16], d[2][16];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int x2 = e & 1, r = e >> 1;
-                    p[e] = ex2(fmaf(__uint_as_float(s[4 * k + e]), c2, KEYS ? nc[x2] : nl[r]));
-                    ds[e] = p[e] * (__uint_as_float(d[4 * k + e]) - (KEYS ? dc[x2] : dl[r]));
-                }
-                if (compare) {
+                        for (int x = 0; x < 2; ++x) {
+                            tmem_ld16x256_x4(tS + 32 * x, s[x]);
+                            tmem_ld16x256_x4(tP + 32 * x, d[x]);
+                        }
+                        tc_wait_ld();
+                        if (compare) {
+                            // the columns that the two rows see, as bits; the thread's 8 k + 2 cg + x at 8 k + x
+                            const int row = u.first + 16 * group + (lane >> 2), off = u.keys - u.rows, end = u.end;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int col = col0 + 8 * k + 2 * cg + (e & 1), r = e >> 1;
-                        const bool seen = KEYS ? ((col >= lo[r] && col < hi[r]) || (col < extra && col >= -off)) : (col < hi[r] && (col >= lo[r] || col < extra));
-                        if (!seen) p[e] = ds[e] = 0.f;
+                            for (int e = 0; e < 2; ++e) {
+                                const int r = row + 8 * e;
+                                uint32_t bits[2];
+                                if (KEY) {
+                                    int lo, hi, full_lo, full_hi;
+                                    rows_of_key(prm.w, r, u.rows, off, lo, hi);
+                                    full_rows(prm.w, u.rows, off, full_lo, full_hi);
+#pragma unroll
+                                    for (int x = 0; x < 2; ++x) {
+                                        const int c0 = col0 + 32 * x;
+                                        bits[x] = (bits_below(hi - c0) & ~bits_below(lo - c0)) | (bits_below(full_hi - c0) & ~bits_below(full_lo - c0));
+                                    }
+                                } else {
+                                    prm.w.seen_bits(r + off, r < end ? u.keys : 0, col0, bits);
+                                }
+#pragma unroll
+                                for (int x = 0; x < 2; ++x) {
+                                    const uint32_t w = bits[x] >> (2 * cg);
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) {
+                                        if (!(w >> (8 * k) & 1u)) s[x][4 * k + 2 * e] = 0xff800000u;
+                                        if (!(w >> (8 * k + 1) & 1u)) s[x][4 * k + 2 * e + 1] = 0xff800000u;
+                                    }
+                                }
+                            }
+                        }
+                        const uint64_t* const st = reinterpret_cast<const uint64_t*>(stats + (M % STAGES) * C::STAT_BYTES) + cg;
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            uint32_t pp[8], pd[8];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                uint64_t cl, cd;
+                                if (KEY) {
+                                    cl = st[4 * (4 * x + k)];
+                                    cd = st[32 + 4 * (4 * x + k)];
+                                }
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const uint64_t sv = pair_of(__uint_as_float(s[x][4 * k + 2 * e]), __uint_as_float(s[x][4 * k + 2 * e + 1]));
+                                    const uint64_t dv = pair_of(__uint_as_float(d[x][4 * k + 2 * e]), __uint_as_float(d[x][4 * k + 2 * e + 1]));
+                                    float2 p = of_pair(fma2(sv, pair_of(c2, c2), KEY ? cl : pair_of(nl[e], nl[e])));
+                                    p.x = ex2(p.x);
+                                    p.y = ex2(p.y);
+                                    if (KEY) pp[2 * k + e] = pack16<TYPE>(p.x, p.y);
+                                    const float2 g = of_pair(mul2(pair_of(p.x, p.y), fma2(dv, pair_of(1.f, 1.f), KEY ? cd : pair_of(nd[e], nd[e]))));
+                                    pd[2 * k + e] = pack16<TYPE>(g.x, g.y);
+                                }
+                            }
+                            // over what this warp has read: the first half's numbers lie in the first quarter of the buffer
+                            if (KEY) tmem_st16x128_x4(tS + 16 * x, pp);
+                            tmem_st16x128_x4(tP + 16 * x, pd);
+                        }
+                    } else {
+                        uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            if (KEY) tmem_st16x128_x4(tS + 16 * x, zero);
+                            tmem_st16x128_x4(tP + 16 * x, zero);
+                        }
                     }
+                    tc_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bP + 8 * set);
                 }
-                pp[2 * k] = pack16<TYPE>(p[0], p[1]);
-                pp[2 * k + 1] = pack16<TYPE>(p[2], p[3]);
-                pd[2 * k] = pack16<TYPE>(ds[0], ds[1]);
-                pd[2 * k + 1] = pack16<TYPE>(ds[2], ds[3]);
-            }
-            if (KEYS) tmem_st16x128_x8(lane_addr + S_COL + 64 * set, pp);
-            tmem_st16x128_x8(lane_addr + DP_COL + 64 * set, pd);
-            tc_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bP + 8 * set);
-        }
-        if (n_items > 0) wait(bD, 0);
-        if (__all_sync(0xffffffffu, !ctl->abort_flag)) {
-            // epilogue: KEYS: half of the warps dK, half dV; else half of dQ's channels each
+            };
+            const bool key = u.key;
+            if (key) element_work(std::true_type());
+            else element_work(std::false_type());
+            // the results: of a key unit half of the warps dK, half dV; of a row unit half of dQ's channels each
+            if (n > 0) wait(bD, n_x & 1);
+            if (!__all_sync(0xffffffffu, !ctl->abort_flag)) break;
             tc_fence_after();
-            constexpr int CH = KEYS ? D / 32 : D / 64;
-            const Rows& to = KEYS && set ? prm.g2 : prm.g1;
-            const float f = KEYS && set ? 1.f : prm.scale;
-            const int ch0 = KEYS ? 0 : set * CH, col = KEYS ? set * D : 0;
-            char* const o_lo = to.row(b, h, row) + 16 * cg + 64 * ch0;
+            const int row = u.first + 16 * group + (lane >> 2);
+            const bool r0 = row < u.end, r1 = row + 8 < u.end;
+            const int chunks = key ? D / 32 : D / 64, ch0 = key ? 0 : set * chunks, col = key ? set * D : 0;
+            const Rows& to = key ? (set ? prm.dv : prm.dk) : prm.dq;
+            const float f = key && set ? 1.f : prm.scale;
+            char* const o_lo = to.row(u.b, u.h, row) + 16 * cg;
             char* const o_hi = o_lo + 16 * to.n;
-#pragma unroll
-            for (int ch = 0; ch < CH; ++ch) {
+            float* const part = u.slot >= 0 ? prm.partial + ((long long)u.slot * 128 + 16 * group + (lane >> 2)) * (2 * D) + col : nullptr;
+            for (int ch = ch0; ch < ch0 + chunks; ++ch) {
                 uint32_t o[16];
-                if (n_items > 0) {
-                    tmem_ld16x256_x4(lane_addr + col + (ch0 + ch) * 32, o);
+                if (n > 0) {
+                    tmem_ld16x256_x4(lane_addr + col + ch * 32, o);
                     tc_wait_ld();
                 } else {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) o[e] = 0u;
+                }
+                if (part) {                              // of a shared-out tile: 32 bits, not scaled
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        __stcg(reinterpret_cast<float2*>(part + 32 * ch + 8 * k + 2 * cg), make_float2(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1])));
+                        __stcg(reinterpret_cast<float2*>(part + 8 * 2 * D + 32 * ch + 8 * k + 2 * cg),
+                               make_float2(__uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3])));
+                    }
+                    continue;
                 }
                 uint32_t w_lo[4], w_hi[4];
 #pragma unroll
@@ -350,7 +607,16 @@ window_back_kernel(const __grid_constant__ CUtensorMap tx1, const __grid_constan
                 const uint4 v_hi = quad_transpose(w_hi[0], w_hi[1], w_hi[2], w_hi[3], cg);
                 if (r0) *reinterpret_cast<uint4*>(o_lo + 64 * ch) = v_lo;
                 if (r1) *reinterpret_cast<uint4*>(o_hi + 64 * ch) = v_hi;
+                __syncwarp();
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (n > 0) mbar_arrive(bDE);
+                mbar_arrive(bUE + 8 * (i & 1));
+            }
+            if (n > 0) ++n_x;
+            N += n;
         }
     }
 
@@ -369,32 +635,70 @@ window_back_kernel(const __grid_constant__ CUtensorMap tx1, const __grid_constan
     }
 }
 
-// lse in base 2 and delta = sum dO O of every query row, padded to whole blocks with rows that have no P.  Bound by HBM: O and dO once.
+// The results of shared-out key tiles, added up in the order of their parts: a thread eight channels of a key's dK or dV.
 template <int D, int TYPE>
-__global__ void __launch_bounds__(256) row_stats_kernel(const Rule w, const Rows out, const Rows dout, const float* lse, float* lse2, float* delta,
+__global__ void __launch_bounds__(256) add_parts_kernel(const __grid_constant__ Params p, int B, int tiles) {
+    grid_dependency_wait();
+    grid_dependency_launch();
+    constexpr int PER_ROW = 2 * D / 8;
+    const int x = blockIdx.x * 256 + threadIdx.x, c = x % PER_ROW, row = x / PER_ROW % 128, t = x / PER_ROW / 128;
+    if (t >= tiles) return;
+    const int heads = B * p.H_kv, tile = t / heads, at = t - tile * heads, b = at / p.H_kv, h = at - b * p.H_kv, key = 128 * tile + row;
+    if (key >= p.w.keys(b)) return;
+    float sum[8] = {};
+    for (int i = 0; i < p.parts; ++i) {
+        const float4* from = reinterpret_cast<const float4*>(p.partial + (((long long)t * p.parts + i) * 128 + row) * (2 * D) + 8 * c);
+        const float4 a = __ldcg(from), bb = __ldcg(from + 1);
+        sum[0] += a.x; sum[1] += a.y; sum[2] += a.z; sum[3] += a.w;
+        sum[4] += bb.x; sum[5] += bb.y; sum[6] += bb.z; sum[7] += bb.w;
+    }
+    const bool value = 8 * c >= D;
+    const float f = value ? 1.f : p.scale;
+    char* to = (value ? p.dv : p.dk).row(b, h, key) + 2 * (8 * c - (value ? D : 0));
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack16<TYPE>(sum[0] * f, sum[1] * f), pack16<TYPE>(sum[2] * f, sum[3] * f),
+                                               pack16<TYPE>(sum[4] * f, sum[5] * f), pack16<TYPE>(sum[6] * f, sum[7] * f));
+}
+
+// Minus log sum exp in base 2 and minus delta of every query row, padded to whole blocks with rows that have no P.  Bound by HBM: O and dO once.
+template <int D, int TYPE>
+__global__ void __launch_bounds__(256) row_stats_kernel(const Rule w, const Rows out, const Rows dout, const float* lse, float* nlse, float* ndelta,
                                                         int H, int padded) {
     constexpr int LPR = D / 8;                           // lanes of a row, 16 bytes each
-    const int lane = threadIdx.x % LPR, i = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, h = blockIdx.y % H, b = blockIdx.y / H;
+    constexpr int AT_ONCE = 4, PER = 256 / LPR;          // rows of a lane, rows of a pass
+    const int lane = threadIdx.x % LPR, i0 = blockIdx.x * (PER * AT_ONCE) + threadIdx.x / LPR, h = blockIdx.y % H, b = blockIdx.y / H;
     grid_dependency_wait();
-    const bool there = i < w.rows(b);
-    float sum = 0.f;
-    if (there) {
-        const uint4 o = __ldcg(reinterpret_cast<const uint4*>(out.row(b, h, i) + 16 * lane)), d = __ldcg(reinterpret_cast<const uint4*>(dout.row(b, h, i) + 16 * lane));
-        const uint32_t ow[4] = {o.x, o.y, o.z, o.w}, dw[4] = {d.x, d.y, d.z, d.w};
+    const int rows = w.rows(b);
+    uint4 o[AT_ONCE], d[AT_ONCE];
+    float l[AT_ONCE];
+#pragma unroll
+    for (int x = 0; x < AT_ONCE; ++x) {
+        const int i = i0 + x * PER;
+        o[x] = d[x] = make_uint4(0, 0, 0, 0);
+        l[x] = -INFINITY;
+        if (i < rows) {
+            o[x] = __ldcg(reinterpret_cast<const uint4*>(out.row(b, h, i) + 16 * lane));
+            d[x] = __ldcg(reinterpret_cast<const uint4*>(dout.row(b, h, i) + 16 * lane));
+            if (lane == 0) l[x] = __ldcg(lse + ((long long)b * H + h) * w.n_q + i);
+        }
+    }
+    grid_dependency_launch();
+#pragma unroll
+    for (int x = 0; x < AT_ONCE; ++x) {
+        const int i = i0 + x * PER;
+        const uint32_t ow[4] = {o[x].x, o[x].y, o[x].z, o[x].w}, dw[4] = {d[x].x, d[x].y, d[x].z, d[x].w};
+        float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float2 a = unpack16<TYPE>(ow[e]), c = unpack16<TYPE>(dw[e]);
             sum = fmaf(a.x, c.x, fmaf(a.y, c.y, sum));
         }
-    }
 #pragma unroll
-    for (int x = 1; x < LPR; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-    grid_dependency_launch();
-    if (lane == 0 && i < padded) {
-        const float l = there ? __ldcg(lse + ((long long)b * H + h) * w.n_q + i) : -INFINITY;
-        const long long at = ((long long)b * H + h) * padded + i;
-        lse2[at] = l == -INFINITY ? INFINITY : l * 1.4426950408889634f;
-        delta[at] = sum;
+        for (int z = 1; z < LPR; z <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, z);
+        if (lane == 0 && i < padded) {
+            const long long at = ((long long)b * H + h) * padded + i;
+            nlse[at] = l[x] == -INFINITY ? -INFINITY : l[x] * -1.4426950408889634f;
+            ndelta[at] = -sum;
+        }
     }
 }
 
@@ -406,13 +710,33 @@ cudaError_t static_init() {
     if (e != cudaSuccess) return e;
     const uint64_t bit = 1ull << (dev & 63);
     if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
-    if ((e = cudaFuncSetAttribute(window_back_kernel<D, TYPE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>())) != cudaSuccess) return e;
-    if ((e = cudaFuncSetAttribute(window_back_kernel<D, TYPE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>())) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(window_back_kernel<D, TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>())) != cudaSuccess) return e;
+    // the warps that take registers wait for them: a build that is launched with fewer would wait for good
+    cudaFuncAttributes attr;
+    if ((e = cudaFuncGetAttributes(&attr, window_back_kernel<D, TYPE>)) != cudaSuccess) return e;
+    if (attr.numRegs * NTHREADS < 32 * (WARPS * ELEMENT_REGS + 4 * LIGHT_REGS)) return cudaErrorInvalidKernelImage;
     done.fetch_or(bit, std::memory_order_release);
     return cudaSuccess;
 }
 
 int padded_rows(const rapid3_window* w) { return (w->n_q + 63) / 64 * 64; }
+int64_t stat_floats(const rapid3_window* w) { return (int64_t)w->B * w->H * padded_rows(w); }
+
+// Tiles of first tokens, and how many units share one: so many that none takes longer than half of what an SM has to do in the mean, all
+// sequences taken as full.
+void sharing(const rapid3_window* w, int& sink_tiles, int& parts) {
+    sink_tiles = 0;
+    parts = 1;
+    if (w->left < 0 || w->n_sink == 0) return;
+    const long long tiles = (w->n_kv + 127) / 128, row_tiles = (w->n_q + 127) / 128, row_blocks = (w->n_q + 63) / 64, key_blocks = (w->n_kv + 63) / 64;
+    sink_tiles = (int)std::min<long long>(tiles, (std::min(w->n_sink, w->n_kv) + 127) / 128);
+    const long long near = (long long)w->left + (w->right < 0 ? std::max(w->n_q, w->n_kv) : w->right) + 192, group = w->H / w->H_kv;
+    const long long sink = group * row_blocks, other = group * std::min(row_blocks, near / 64);
+    const long long total = (long long)w->B * w->H_kv * (sink_tiles * sink + (tiles - sink_tiles) * other) +
+                            (long long)w->B * w->H * row_tiles * std::min(key_blocks, near / 64 + (w->n_sink + 63) / 64);
+    const long long most = std::max<long long>(48, total / SM_COUNT / 2), slots = (long long)sink_tiles * w->B * w->H_kv;
+    parts = (int)std::min<long long>(std::min<long long>(MAX_PARTS, (sink + most - 1) / most), std::max<long long>(1, MAX_SLOTS / slots));
+}
 
 template <int D, int TYPE>
 int run(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, const rapid3_rows* v, const rapid3_rows* out, const float* lse,
@@ -429,26 +753,37 @@ int run(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, cons
     Params p;
     p.w = rule_of(w);
     p.padded = padded_rows(w);
-    float* const delta = stats + (size_t)w->B * w->H * p.padded;
-    p.lse2 = stats;
-    p.delta = delta;
+    float* const ndelta = stats + stat_floats(w);
+    p.nlse = stats;
+    p.ndelta = ndelta;
+    p.partial = ndelta + stat_floats(w);
     p.H = w->H;
     p.H_kv = w->H_kv;
     p.group = w->H / w->H_kv;
     p.scale = w->softmax_scale;
     p.scale_log2 = w->softmax_scale * 1.4426950408889634f;
-    constexpr int PER = 256 / (D / 8);
-    if (launch_kernel(row_stats_kernel<D, TYPE>, dim3((p.padded + PER - 1) / PER, w->B * w->H), dim3(256), 0, s, p.w, rows_arg(out), rows_arg(dout), lse,
-                      stats, delta, w->H, p.padded) != cudaSuccess)
+    p.dq = rows_arg(dq);
+    p.dk = rows_arg(dk);
+    p.dv = rows_arg(dv);
+    p.key_tiles = (w->n_kv + 127) / 128;
+    p.row_tiles = (w->n_q + 127) / 128;
+    sharing(w, p.sink_tiles, p.parts);
+    const long long full = std::min<long long>(w->n_q, w->n_full ? (long long)w->n_full + w->n_q - w->n_kv : 0);    // rows, of full sequences
+    p.full_tiles = full > 0 ? (int)((full + 127) / 128) : 0;
+    p.last_first = w->left < 0 && w->right >= 0;
+    const int key_heads = w->B * w->H_kv, heads = w->B * w->H;
+    p.sink_units = key_heads * p.sink_tiles * p.parts;
+    p.key_units = p.sink_units + key_heads * (p.key_tiles - p.sink_tiles);
+    p.full_units = p.key_units + heads * p.full_tiles;
+    const int units = p.full_units + heads * (p.row_tiles - p.full_tiles);
+    constexpr int PER = 4 * 256 / (D / 8);
+    if (launch_kernel(row_stats_kernel<D, TYPE>, dim3((p.padded + PER - 1) / PER, heads), dim3(256), 0, s, p.w, rows_arg(out), rows_arg(dout), lse,
+                      stats, ndelta, w->H, p.padded) != cudaSuccess)
         return RAPID3_ERR_CUDA;
-    p.g1 = rows_arg(dk);
-    p.g2 = rows_arg(dv);
-    p.tiles = (w->n_kv + 127) / 128;
-    if (launch_kernel(window_back_kernel<D, TYPE, true>, dim3(w->B * w->H_kv * p.tiles), dim3(NTHREADS), smem_bytes<D>(), s, tk, tv, tq, td, p) != cudaSuccess)
+    if (launch_kernel(window_back_kernel<D, TYPE>, dim3(units), dim3(NTHREADS), smem_bytes<D>(), s, tq, tk, tv, td, p, w->B) != cudaSuccess)
         return RAPID3_ERR_CUDA;
-    p.g1 = p.g2 = rows_arg(dq);
-    p.tiles = (w->n_q + 127) / 128;
-    if (launch_kernel(window_back_kernel<D, TYPE, false>, dim3(w->B * w->H * p.tiles), dim3(NTHREADS), smem_bytes<D>(), s, tq, td, tk, tv, p) != cudaSuccess)
+    const int shared = key_heads * p.sink_tiles;
+    if (p.parts > 1 && launch_kernel(add_parts_kernel<D, TYPE>, dim3((shared * 128 * (2 * D / 8) + 255) / 256), dim3(256), 0, s, p, w->B, shared) != cudaSuccess)
         return RAPID3_ERR_CUDA;
     return RAPID3_OK;
 }
@@ -465,7 +800,11 @@ extern "C" {
 
 int64_t rapid3_window_workspace_bytes(const rapid3_window* w) {
     const int r = window::check(w);
-    return r ? r : (int64_t)w->B * w->H * padded_rows(w) * 2 * sizeof(float);
+    if (r) return r;
+    int sink_tiles, parts;
+    sharing(w, sink_tiles, parts);
+    const int64_t slots = parts > 1 ? (int64_t)w->B * w->H_kv * sink_tiles * parts : 0;
+    return (2 * stat_floats(w) + slots * 128 * 2 * w->D) * sizeof(float);
 }
 
 int rapid3_window_attn_backward(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, const rapid3_rows* v, const rapid3_rows* out,

@@ -29,6 +29,8 @@ PROMPTS = [  # type, B, H, Hkv, D, n_q, n_kv, left, right, sink, full, q_len, kv
     ("f16", 3, 20, 4, 128, 650, 650, 200, 200, 64, 64, [650, 649, 1], [650, 649, 1], "tokens"),
     ("bf16", 2, 39, 13, 128, 300, 300, 80, 0, 0, 0, None, None, "heads"),                # an odd number of heads for each key head: 256 rows a unit
     ("bf16", 1, 39, 13, 64, 1500, 1500, 300, 0, 10, 0, [1400], [1450], "heads"),
+    ("f16", 1, 16, 1, 128, 1100, 1100, 99, 0, 4, 0, None, None, "heads"),                # gradients: many units for the one tile of first tokens
+    ("bf16", 2, 32, 1, 64, 900, 1000, 40, 5, 130, 0, [900, 60], [1000, 140], "tokens"),  # and for two, of sequences that fill few of them
 ]
 
 
