@@ -369,18 +369,23 @@ def _rows(t: Optional[torch.Tensor]):
     return Rows(t.data_ptr(), sb, sh, sn)
 
 
-def _check_tensors(what: str, like: torch.Tensor, tensors):
-    """Each (name, tensor, shape): on `like`'s device, which is the current one, of its type and that shape, channels adjacent."""
-    if not like.is_cuda or like.get_device() != torch._C._cuda_getDevice():
+# The checks of the calls below cost a third of a small call on the host (13 us when they were written for brevity): tensor by tensor, each
+# attribute read once, and what is wrong said only when something is.
+def _device(what: str, like: torch.Tensor) -> int:
+    dev = like.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
         raise ValueError(f"{what}: tensors must be on the current CUDA device")
-    for name, t, shape in tensors:
-        if t is None or t.dtype != like.dtype or t.device != like.device or t.shape != shape or (t.stride(-1) != 1 and shape[-1] > 1):
-            raise ValueError(f"{what}: {name} must be {tuple(shape)} of {like.dtype} on {like.device} with adjacent channels")
+    return dev
 
 
-def _check_vector(what: str, name: str, t: Optional[torch.Tensor], n: int, like: torch.Tensor, dtype=torch.float32):
-    if t is None or t.dtype != dtype or t.device != like.device or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what}: {name} must be {n} contiguous values of {dtype} on {like.device}")
+def _check_like(what: str, name: str, t: Optional[torch.Tensor], dtype: torch.dtype, dev: int, shape):
+    if t is None or t.dtype is not dtype or t.get_device() != dev or t.shape != shape or t.stride(3) != 1:
+        raise ValueError(f"{what}: {name} must be {tuple(shape)} of {dtype} on CUDA device {dev} with adjacent channels")
+
+
+def _check_vector(what: str, name: str, t: Optional[torch.Tensor], n: int, dev: int, dtype=torch.float32):
+    if t is None or t.dtype is not dtype or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be {n} contiguous values of {dtype} on CUDA device {dev}")
 
 
 def rapid3_rotary_freqs(channels: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: int = 1,
@@ -416,26 +421,36 @@ class Rotary:
         if len(pairs) > axes or sum(pairs) != freq.numel() or min(pairs) < 0:
             raise ValueError("Rotary: axis_pairs must be one count for each axis, freq's length in all")
         pairs += [0] * (4 - len(pairs))
-        self.freq, self.pos, self.device = freq, pos, freq.device
+        self.freq, self.pos, self.device = freq, pos, freq.get_device()
         self.B, self.N = (0, 0) if pos is None else pos.shape[:2]
         self.turn = Turn(0 if layout == "pairs" else 1, 2 * freq.numel(), axes, (ctypes.c_int32 * 4)(*pairs), freq.data_ptr(), _ptr(pos),
                          0 if pos is None or self.B == 1 else pos.stride(0), 0 if pos is None or self.N == 1 else pos.stride(1), int(pos0),
                          float(amplitude))
 
-    def check(self, what: str, like: torch.Tensor):
-        B, _, N, _ = like.shape
-        if self.device != like.device or (self.pos is not None and (self.N != N or self.B not in (1, B))):
-            raise ValueError(f"{what}: the positions are those of {self.B} x {self.N} tokens on {self.device}, not of {B} x {N} on {like.device}")
+    def check(self, what: str, dev: int, B: int, N: int):
+        if self.device != dev or (self.pos is not None and (self.N != N or (self.B != 1 and self.B != B))):
+            raise ValueError(f"{what}: the positions are those of {self.B} x {self.N} tokens on CUDA device {self.device}, not of {B} x {N} on {dev}")
 
 
-def _heads(what: str, q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, others):
-    """The shape of Q and K (k may be None), after checking them and `others`, (name, tensor, which of the two it is like)."""
-    if q.dim() != 4 or q.dtype not in _TYPES or (k is not None and (k.dim() != 4 or k.shape[0] != q.shape[0] or k.shape[2:] != q.shape[2:])):
-        raise ValueError(f"{what}: q and k must be [B, H, N, D] of bf16, fp16 or fp32 and differ in H only")
-    rotary.check(what, q)
-    _check_tensors(what, q, [("q", q, q.shape)] + ([] if k is None else [("k", k, k.shape)]) +
-                   [(name, t, (q if w == 0 else k).shape) for name, t, w in others if w == 0 or k is not None])
-    return Heads(_TYPES[q.dtype], q.shape[0], q.shape[2], q.shape[3], q.shape[1], 0 if k is None else k.shape[1])
+def _heads(what: str, q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, like_q, like_k):
+    """The shape of Q and K (k may be None), after checking them and what is like them: (name, tensor)s.  Also the device."""
+    shape, dtype, dev = q.shape, q.dtype, _device(what, q)
+    kind = _TYPES.get(dtype)
+    if kind is None or len(shape) != 4:
+        raise ValueError(f"{what}: q must be [B, H, N, D] of bf16, fp16 or fp32")
+    B, H, N, D = shape
+    rotary.check(what, dev, B, N)
+    _check_like(what, "q", q, dtype, dev, shape)
+    for name, t in like_q:
+        _check_like(what, name, t, dtype, dev, shape)
+    Hk = 0
+    if k is not None:
+        k_shape = k.shape
+        Hk = k_shape[1] if len(k_shape) == 4 else 0
+        _check_like(what, "k", k, dtype, dev, (B, Hk, N, D))
+        for name, t in like_k:
+            _check_like(what, name, t, dtype, dev, k_shape)
+    return Heads(kind, B, N, D, H, Hk), dev
 
 
 def rapid3_rotary(q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, q_out: Optional[torch.Tensor] = None,
@@ -444,7 +459,7 @@ def rapid3_rotary(q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, q_
     backward: q and k are gradients of the outputs, and those of the inputs come back."""
     q_out = torch.empty_like(q) if q_out is None else q_out
     k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
-    shape = _heads("rapid3_rotary", q, k, rotary, (("q_out", q_out, 0), ("k_out", k_out, 1)))
+    shape, _ = _heads("rapid3_rotary", q, k, rotary, (("q_out", q_out),), (("k_out", k_out),))
     _check(load().rapid3_rotary(shape, _rows(q), _rows(k), rotary.turn, int(backward), _rows(q_out), None if k is None else _rows(k_out), _stream()),
            "rapid3_rotary")
     return q_out, k_out
@@ -456,10 +471,10 @@ def rapid3_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_gain: torch
     what = "rapid3_norm_rotary"
     q_out = torch.empty_like(q) if q_out is None else q_out
     k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
-    shape = _heads(what, q, k, rotary, (("q_out", q_out, 0), ("k_out", k_out, 1)))
-    _check_vector(what, "q_gain", q_gain, q.shape[3], q)
+    shape, dev = _heads(what, q, k, rotary, (("q_out", q_out),), (("k_out", k_out),))
+    _check_vector(what, "q_gain", q_gain, shape.D, dev)
     if k is not None:
-        _check_vector(what, "k_gain", k_gain, q.shape[3], q)
+        _check_vector(what, "k_gain", k_gain, shape.D, dev)
     _check(load().rapid3_norm_rotary(shape, _rows(q), _rows(k), _ptr(q_gain), _ptr(k_gain), float(eps), rotary.turn, _rows(q_out),
                                      None if k is None else _rows(k_out), _stream()), what)
     return q_out, k_out
@@ -476,9 +491,9 @@ def rapid3_norm_rotary_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Ten
     dk = torch.empty_like(k) if dk is None and k is not None else dk
     dq_gain = torch.empty_like(q_gain) if dq_gain is None else dq_gain
     dk_gain = torch.empty_like(k_gain) if dk_gain is None and k is not None and k_gain is not None else dk_gain
-    shape = _heads(what, q, k, rotary, (("dq_out", dq_out, 0), ("dk_out", dk_out, 1), ("dq", dq, 0), ("dk", dk, 1)))
+    shape, dev = _heads(what, q, k, rotary, (("dq_out", dq_out), ("dq", dq)), (("dk_out", dk_out), ("dk", dk)))
     for name, t in (("q_gain", q_gain), ("dq_gain", dq_gain)) + ((("k_gain", k_gain), ("dk_gain", dk_gain)) if k is not None else ()):
-        _check_vector(what, name, t, q.shape[3], q)
+        _check_vector(what, name, t, shape.D, dev)
     lib = load()
     size = lib.rapid3_norm_rotary_workspace_bytes(shape)
     workspace = torch.empty(max(16, size), dtype=torch.uint8, device=q.device)
@@ -488,22 +503,31 @@ def rapid3_norm_rotary_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Ten
     return dq, dk, dq_gain, dk_gain
 
 
-def _window(what: str, q: torch.Tensor, k: torch.Tensor, others, left: int, right: int, n_sink: int, n_full: int,
+def _window(what: str, q: torch.Tensor, k: torch.Tensor, like_q, like_k, left: int, right: int, n_sink: int, n_full: int,
             q_len: Optional[torch.Tensor], kv_len: Optional[torch.Tensor], softmax_scale: Optional[float]):
-    """The shape and rule of a windowed attention, after checking Q, K, the lengths and `others`, (name, tensor, which of the two it is like)."""
-    if q.dim() != 4 or k.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float16) or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
-        raise ValueError(f"{what}: q [B, H, n_q, D] and k [B, H_kv, n_kv, D] must be bf16 or fp16 and agree in B and D")
-    _check_tensors(what, q, [("q", q, q.shape), ("k", k, k.shape)] + [(name, t, (q if w == 0 else k).shape) for name, t, w in others])
-    for name, t in (("q_len", q_len), ("kv_len", kv_len)):
-        if t is not None:
-            _check_vector(what, name, t, q.shape[0], q, torch.int32)
-    return Window(_TYPES[q.dtype], q.shape[0], q.shape[1], k.shape[1], q.shape[3], q.shape[2], k.shape[2], int(left), int(right), int(n_sink),
-                  int(n_full), float(softmax_scale if softmax_scale is not None else q.shape[3] ** -0.5), _ptr(q_len), _ptr(kv_len))
+    """The shape and rule of a windowed attention, after checking Q, K, the lengths and what is like Q and K: (name, tensor)s.  Also the device."""
+    shape, k_shape, dtype, dev = q.shape, k.shape, q.dtype, _device(what, q)
+    if len(shape) != 4 or len(k_shape) != 4 or (dtype is not torch.bfloat16 and dtype is not torch.float16):
+        raise ValueError(f"{what}: q [B, H, n_q, D] and k [B, H_kv, n_kv, D] must be bf16 or fp16")
+    B, H, n_q, D = shape
+    _, Hk, n_kv, _ = k_shape
+    _check_like(what, "q", q, dtype, dev, shape)
+    _check_like(what, "k", k, dtype, dev, (B, Hk, n_kv, D))
+    for name, t in like_q:
+        _check_like(what, name, t, dtype, dev, shape)
+    for name, t in like_k:
+        _check_like(what, name, t, dtype, dev, k_shape)
+    if q_len is not None:
+        _check_vector(what, "q_len", q_len, B, dev, torch.int32)
+    if kv_len is not None:
+        _check_vector(what, "kv_len", kv_len, B, dev, torch.int32)
+    return Window(_TYPES[dtype], B, H, Hk, D, n_q, n_kv, int(left), int(right), int(n_sink), int(n_full),
+                  float(softmax_scale if softmax_scale is not None else D ** -0.5), _ptr(q_len), _ptr(kv_len)), dev
 
 
-def _check_lse(what: str, lse: Optional[torch.Tensor], q: torch.Tensor):
-    if lse is None or lse.dtype != torch.float32 or lse.device != q.device or lse.shape != q.shape[:3] or not lse.is_contiguous():
-        raise ValueError(f"{what}: lse must be contiguous fp32 {tuple(q.shape[:3])} on {q.device}")
+def _check_lse(what: str, lse: Optional[torch.Tensor], q: torch.Tensor, dev: int):
+    if lse is None or lse.dtype is not torch.float32 or lse.get_device() != dev or lse.shape != q.shape[:3] or not lse.is_contiguous():
+        raise ValueError(f"{what}: lse must be contiguous fp32 {tuple(q.shape[:3])} on CUDA device {dev}")
 
 
 def rapid3_window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
@@ -514,9 +538,9 @@ def rapid3_window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: O
     Returns out (allocated, rows from q_len on unset, unless given) and lse (filled if given)."""
     what = "rapid3_window_attn"
     out = torch.empty_like(q) if out is None else out
-    shape = _window(what, q, k, (("v", v, 1), ("out", out, 0)), left, right, n_sink, n_full, q_len, kv_len, softmax_scale)
+    shape, dev = _window(what, q, k, (("out", out),), (("v", v),), left, right, n_sink, n_full, q_len, kv_len, softmax_scale)
     if lse is not None:
-        _check_lse(what, lse, q)
+        _check_lse(what, lse, q, dev)
     _check(load().rapid3_window_attn(shape, _rows(q), _rows(k), _rows(v), _rows(out), _ptr(lse), _stream()), what)
     return out, lse
 
@@ -529,9 +553,9 @@ def rapid3_window_attn_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     Rows from q_len and keys from kv_len on are left as they were.  The same call gives the same bits."""
     what = "rapid3_window_attn_backward"
     dq, dk, dv = (torch.empty_like(x) if g is None else g for x, g in ((q, dq), (k, dk), (v, dv)))
-    shape = _window(what, q, k, (("v", v, 1), ("out", out, 0), ("dout", dout, 0), ("dq", dq, 0), ("dk", dk, 1), ("dv", dv, 1)), left, right, n_sink,
-                    n_full, q_len, kv_len, softmax_scale)
-    _check_lse(what, lse, q)
+    shape, dev = _window(what, q, k, (("out", out), ("dout", dout), ("dq", dq)), (("v", v), ("dk", dk), ("dv", dv)), left, right, n_sink, n_full,
+                         q_len, kv_len, softmax_scale)
+    _check_lse(what, lse, q, dev)
     lib = load()
     size = lib.rapid3_window_workspace_bytes(shape)
     workspace = torch.empty(max(16, size), dtype=torch.uint8, device=q.device)

@@ -7,10 +7,12 @@
 // All of it in fp32, one rounding to the tensors' type.  The angles of far positions need more: position * freq / 2 pi is taken in
 // fp64, its fraction alone goes on to sincospif.
 //
-// Bound by HBM: a row is read once (BACK with NORM: two rows) and written once.  A lane holds four channel pairs, so the rotation is
-// the lane's own in both layouts; the lanes of a row add up its squares by shuffles.  A thread block does TOKENS tokens of one
-// sequence for many heads, which share the tokens' cosines and sines: these are computed once, into shared memory, while the first rows
-// are on their way (for 48 heads 4 % of the instructions; from a table in memory they would be a second read of up to a row a token).
+// Bound by HBM: a row is read once (BACK with NORM: two rows) and written once, so that what counts besides is how few instructions a
+// row takes.  A group of lanes holds a row, a lane four channel pairs, so the rotation is the lane's own in both layouts and the lanes of a row
+// add up its squares by shuffles.  A group stays with one token and goes through its heads: cosines and sines, times the gains where
+// both are factors, are computed once and stay in registers, and the arithmetic goes in packed pairs.  The rows come by asynchronous copies
+// through a ring of the warp's own in shared memory, DEPTH of them on their way (in registers, with as many warps as these allow, no more than
+// 32 to 64 KB an SM were, and the kernel waited for memory half of the time).
 #include <math.h>
 
 #include <cuda_bf16.h>
@@ -19,10 +21,16 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "ptx.cuh"
 
 namespace {
 
-constexpr int WARPS = 8, TOKENS = 16, MAX_D = 256, MAX_AXES = 4;
+using ptx::fma2;
+using ptx::mul2;
+using ptx::of_pair;
+using ptx::pair_of;
+
+constexpr int WARPS = 8, MAX_D = 256, MAX_AXES = 4;
 constexpr int GRAD_BLOCKS_PER_SM = 4;                   // thread blocks of a backward launch: each leaves one partial sum of the gains' gradients
 constexpr int MAX_GRAD_BLOCKS = GRAD_BLOCKS_PER_SM * SM_COUNT;
 
@@ -47,210 +55,333 @@ struct TurnArg {
 struct Args {
     RowsArg t[2];                // Q, K
     TurnArg turn;
-    float eps;
+    float eps, inv_D;
     int N, D, log_tokens, tiles; // tokens of a thread block (a power of two), thread blocks of a sequence
     int n_tiles;                 // of all sequences
     int heads_per_block;
     float* partial;              // BACK with NORM: [thread block][2][D]
 };
 
-// Four consecutive channels, widened.
+// A lane's eight channels of a row, as they lie in memory: two runs of four.
 template <int TYPE>
-__device__ __forceinline__ void load4(const char* p, float (&x)[4]) {
+struct Raw {
+    uint2 lo, hi;
+};
+template <>
+struct Raw<RAPID3_F32> {
+    uint4 lo, hi;
+};
+template <int TYPE, bool HALVES>
+__device__ __forceinline__ Raw<TYPE> read_raw(const char* p, int at0, int at1) {
+    Raw<TYPE> r;
     if constexpr (TYPE == RAPID3_F32) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
-        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+        r.lo = *reinterpret_cast<const uint4*>(p + 4 * at0);
+        r.hi = *reinterpret_cast<const uint4*>(p + 4 * at1);
+    } else if constexpr (HALVES) {
+        r.lo = *reinterpret_cast<const uint2*>(p + 2 * at0);
+        r.hi = *reinterpret_cast<const uint2*>(p + 2 * at1);
     } else {
-        const uint2 v = __ldcg(reinterpret_cast<const uint2*>(p));
-        if constexpr (TYPE == RAPID3_BF16) {
-            x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
-            x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
-        } else {
-            const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&v.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
-            x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
-        }
+        const uint4 v = *reinterpret_cast<const uint4*>(p + 2 * at0);   // the two runs lie side by side
+        r.lo = make_uint2(v.x, v.y);
+        r.hi = make_uint2(v.z, v.w);
     }
+    return r;
+}
+// 16 bytes to shared memory, past the L1; zeros where there is nothing to read.
+__device__ __forceinline__ void copy16(uint32_t to, const char* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 template <int TYPE>
-__device__ __forceinline__ void store4(char* p, float a, float b, float c, float d) {
-    if constexpr (TYPE == RAPID3_F32) {
-        *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
-    } else if constexpr (TYPE == RAPID3_BF16) {
-        const __nv_bfloat162 u = __floats2bfloat162_rn(a, b), v = __floats2bfloat162_rn(c, d);
-        *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
-    } else {
-        const __half2 u = __floats2half2_rn(a, b), v = __floats2half2_rn(c, d);
-        *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
+__device__ __forceinline__ float2 wide2(uint32_t v) {
+    if constexpr (TYPE == RAPID3_BF16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2*>(&v));
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t narrow2(float a, float b) {
+    if constexpr (TYPE == RAPID3_BF16) {
+        const __nv_bfloat162 u = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&u);
     }
+    const __half2 u = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&u);
+}
+// Four channel pairs, packed by twos: first members a, second members b.
+struct Pairs {
+    uint64_t a[2], b[2];
+};
+template <int TYPE, bool HALVES>
+__device__ __forceinline__ Pairs widen(const Raw<TYPE>& r) {
+    float2 w[4];                                         // the lane's eight channels in order
+    if constexpr (TYPE == RAPID3_F32) {
+        w[0] = make_float2(__uint_as_float(r.lo.x), __uint_as_float(r.lo.y));
+        w[1] = make_float2(__uint_as_float(r.lo.z), __uint_as_float(r.lo.w));
+        w[2] = make_float2(__uint_as_float(r.hi.x), __uint_as_float(r.hi.y));
+        w[3] = make_float2(__uint_as_float(r.hi.z), __uint_as_float(r.hi.w));
+    } else {
+        w[0] = wide2<TYPE>(r.lo.x);
+        w[1] = wide2<TYPE>(r.lo.y);
+        w[2] = wide2<TYPE>(r.hi.x);
+        w[3] = wide2<TYPE>(r.hi.y);
+    }
+    Pairs p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        p.a[i] = HALVES ? pair_of(w[i].x, w[i].y) : pair_of(w[2 * i].x, w[2 * i + 1].x);
+        p.b[i] = HALVES ? pair_of(w[2 + i].x, w[2 + i].y) : pair_of(w[2 * i].y, w[2 * i + 1].y);
+    }
+    return p;
+}
+template <int TYPE, bool HALVES>
+__device__ __forceinline__ void store_pairs(char* p, int at0, int at1, const Pairs& z) {
+    const float2 a0 = of_pair(z.a[0]), a1 = of_pair(z.a[1]), b0 = of_pair(z.b[0]), b1 = of_pair(z.b[1]);
+    if constexpr (TYPE == RAPID3_F32) {
+        *reinterpret_cast<float4*>(p + 4 * at0) = HALVES ? make_float4(a0.x, a0.y, a1.x, a1.y) : make_float4(a0.x, b0.x, a0.y, b0.y);
+        *reinterpret_cast<float4*>(p + 4 * at1) = HALVES ? make_float4(b0.x, b0.y, b1.x, b1.y) : make_float4(a1.x, b1.x, a1.y, b1.y);
+    } else if constexpr (HALVES) {
+        *reinterpret_cast<uint2*>(p + 2 * at0) = make_uint2(narrow2<TYPE>(a0.x, a0.y), narrow2<TYPE>(a1.x, a1.y));
+        *reinterpret_cast<uint2*>(p + 2 * at1) = make_uint2(narrow2<TYPE>(b0.x, b0.y), narrow2<TYPE>(b1.x, b1.y));
+    } else {
+        *reinterpret_cast<uint4*>(p + 2 * at0) = make_uint4(narrow2<TYPE>(a0.x, b0.x), narrow2<TYPE>(a0.y, b0.y), narrow2<TYPE>(a1.x, b1.x), narrow2<TYPE>(a1.y, b1.y));
+    }
+}
+__device__ __forceinline__ uint64_t twice(float x) { return pair_of(x, x); }
+// Sum of squares, or of products, of a lane's eight numbers.
+__device__ __forceinline__ float dot8(const Pairs& x, const Pairs& y) {
+    const float2 s = of_pair(fma2(x.a[0], y.a[0], fma2(x.a[1], y.a[1], fma2(x.b[0], y.b[0], mul2(x.b[1], y.b[1])))));
+    return s.x + s.y;
 }
 
-// LPR lanes hold a row: lane c the channel pairs 4 c .. 4 c + 3, a their first members and b their second ones.
+// Rows of a lane group on their way at once.
+__host__ __device__ constexpr int depth_of(int type, bool grads) { return type == RAPID3_F32 ? (grads ? 3 : 4) : grads ? 6 : 8; }
+__host__ __device__ constexpr size_t ring_bytes(int type, bool grads) { return (size_t)WARPS * depth_of(type, grads) * (grads ? 2 : 1) * 256 * (type == RAPID3_F32 ? 4 : 2); }
+
+// LPR lanes hold a row: lane c the channel pairs 4 c .. 4 c + 3.
 template <int TYPE, int LPR, bool HALVES, bool NORM, bool BACK>
 __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constant__ Args p) {
-    constexpr int RPW = 32 / LPR, SIZE = TYPE == RAPID3_F32 ? 4 : 2;
+    constexpr int RPW = 32 / LPR, SLOTS = WARPS * RPW;   // rows of a warp, of a thread block, at a time
     constexpr bool GRADS = NORM && BACK;
-    constexpr int AHEAD = GRADS ? 2 : 4;                // rows of a lane on their way at once
-    extern __shared__ float4 table[];                   // [token][cos, sin][LPR]: four pairs; unturned ones (1, 0)
-    __shared__ float sums[GRADS ? WARPS : 1][GRADS ? 2 * MAX_D : 1];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = lane % LPR, r0 = lane / LPR;
+    constexpr int SIZE = TYPE == RAPID3_F32 ? 4 : 2, DEPTH = depth_of(TYPE, GRADS), STREAMS = GRADS ? 2 : 1, U = NORM && !BACK ? DEPTH / 2 : 1;
+    constexpr int ROW = 8 * LPR * SIZE, STEP = 256 * SIZE;              // bytes of a row's place, of a warp's rows
+    extern __shared__ __align__(16) char ring[];        // [warp][DEPTH][x, dz][row of the warp]
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = lane % LPR, slot = warp * RPW + lane / LPR;
     const int D = p.D, half = p.turn.pairs;
     const bool here = 8 * c < D;
     // the lane's channels: two runs of four
     const bool split = HALVES && 4 * c < half;
     const int at0 = split ? 4 * c : 8 * c, at1 = split ? half + 4 * c : 8 * c + 4;
-    float acc[GRADS ? 2 : 1][8];
+    Pairs acc[GRADS ? 2 : 1];
 #pragma unroll
-    for (int w = 0; w < (GRADS ? 2 : 1); ++w)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[w][e] = 0.f;
+    for (int w = 0; w < (GRADS ? 2 : 1); ++w) acc[w].a[0] = acc[w].a[1] = acc[w].b[0] = acc[w].b[1] = 0ull;
+    // the slot's token of a tile, and its share of the heads
+    const int mine = slot & ((1 << p.log_tokens) - 1), head0 = slot >> p.log_tokens, head_step = SLOTS >> p.log_tokens;
+    char* const ring_at = ring + warp * (DEPTH * STREAMS * STEP) + (lane / LPR) * ROW;
+    const uint32_t my_ring = ptx::smem_u32(ring_at);
     grid_dependency_wait();
     for (int tile = blockIdx.x; tile < p.n_tiles; tile += gridDim.x) {
-        const int b = tile / p.tiles, n0 = (tile - b * p.tiles) << p.log_tokens, tokens = min(1 << p.log_tokens, p.N - n0);
-        __syncthreads();                                // the tile before is through with the table
-        for (int x = threadIdx.x; x < tokens * 4 * LPR; x += 32 * WARPS) {
-            const int t = x / (4 * LPR), pair = x % (4 * LPR);
-            float sine = 0.f, cosine = 1.f;
-            if (pair < half) {
-                int axis = 0;
-                while (axis + 1 < p.turn.axes && pair >= p.turn.axis_end[axis]) ++axis;
-                const int at = p.turn.pos ? __ldcg(p.turn.pos + b * p.turn.pos_b + (n0 + t) * p.turn.pos_n + axis) : p.turn.pos0 + n0 + t;
-                double turns = (double)at * (__ldcg(p.turn.freq + pair) * 0.15915494309189533577);
-                turns -= rint(turns);
-                sincospif(2.f * (float)turns, &sine, &cosine);
-                sine *= p.turn.amplitude;
-                cosine *= p.turn.amplitude;
-            }
-            float* to = reinterpret_cast<float*>(table + (t * 2) * LPR + pair / 4) + pair % 4;
-            to[0] = cosine;
-            to[4 * LPR] = BACK ? -sine : sine;          // the transposed rotation turns back
+        const int b = tile / p.tiles, n = ((tile - b * p.tiles) << p.log_tokens) + mine;
+        const bool live = n < p.N && here;
+        // this thread block's heads among those of Q and then K; a slot's steps through them
+        int first_head[2], heads[2], steps[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int before = w ? p.t[0].H : 0;
+            first_head[w] = max(0, (int)blockIdx.y * p.heads_per_block - before);
+            heads[w] = max(0, min(p.t[w].H, ((int)blockIdx.y + 1) * p.heads_per_block - before) - first_head[w]);
+            steps[w] = (heads[w] + head_step - 1) / head_step;
         }
-        __syncthreads();
+        // the copies, Q's rows and then K's
+        const char *in = nullptr, *grad = nullptr;
+        long long in_step = 0, grad_step = 0;
+        int issued = 0, coming = 0;                      // heads of the tensor that the slot has still to fetch: this many / head_step, rounded up
+        auto source = [&](int w) {
+            const RowsArg& t = p.t[w];
+            const int h = (w ? first_head[1] : first_head[0]) + head0;
+            coming = n < p.N ? (w ? heads[1] : heads[0]) - head0 : 0;
+            in = t.in + b * t.in_b + h * t.in_h + n * t.in_n;
+            in_step = t.in_h * head_step;
+            if constexpr (GRADS) {
+                grad = t.grad + b * t.grad_b + h * t.grad_h + n * t.grad_n;
+                grad_step = t.grad_h * head_step;
+            }
+        };
+        source(steps[0] > 0 ? 0 : 1);
+        auto issue = [&]() {
+            if (issued < steps[0] + steps[1]) {
+                if (issued == steps[0] && issued > 0) source(1);
+                const uint32_t to = my_ring + (issued % DEPTH) * (STREAMS * STEP);
+#pragma unroll
+                for (int k = 0; k < SIZE / 2; ++k) {     // (lanes side by side fetch pieces side by side)
+                    const int piece = c + k * LPR;
+                    const bool there = coming > 0 && piece * 16 < D * SIZE;
+                    copy16(to + 16 * piece, there ? in + 16 * piece : reinterpret_cast<const char*>(p.t[0].in), there);
+                    if constexpr (GRADS) copy16(to + STEP + 16 * piece, there ? grad + 16 * piece : reinterpret_cast<const char*>(p.t[0].in), there);
+                }
+                coming -= head_step;
+                in += in_step;
+                if constexpr (GRADS) grad += grad_step;
+            }
+            ++issued;
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        for (int u = 0; u < DEPTH; ++u) issue();
+        int step = 0;
+        Pairs cs, sn;                                    // of the first and second members alike
+        {
+            float cosine[4], sine[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int pair = 4 * c + i;
+                cosine[i] = 1.f;
+                sine[i] = 0.f;
+                if (pair < half && live) {
+                    int axis = 0;
+                    while (axis + 1 < p.turn.axes && pair >= p.turn.axis_end[axis]) ++axis;
+                    const int at = p.turn.pos ? __ldcg(p.turn.pos + b * p.turn.pos_b + n * p.turn.pos_n + axis) : p.turn.pos0 + n;
+                    double turns = (double)at * (__ldcg(p.turn.freq + pair) * 0.15915494309189533577);
+                    turns -= rint(turns);
+                    sincospif(2.f * (float)turns, &sine[i], &cosine[i]);
+                    sine[i] *= BACK ? -p.turn.amplitude : p.turn.amplitude;     // the transposed rotation turns back
+                    cosine[i] *= p.turn.amplitude;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                cs.a[i] = cs.b[i] = pair_of(cosine[2 * i], cosine[2 * i + 1]);
+                sn.a[i] = pair_of(sine[2 * i], sine[2 * i + 1]);
+                sn.b[i] = pair_of(-sine[2 * i], -sine[2 * i + 1]);
+            }
+        }
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             const RowsArg& t = p.t[w];
-            // this thread block's heads among those of Q and then K
-            const int before = w ? p.t[0].H : 0;
-            const int h0 = max(0, (int)blockIdx.y * p.heads_per_block - before), h1 = min(t.H, ((int)blockIdx.y + 1) * p.heads_per_block - before);
-            const int rows = h1 > h0 ? (h1 - h0) << p.log_tokens : 0;
-            if (rows == 0) continue;
-            float ga[4], gb[4];
+            if (heads[w] == 0) continue;
+            Pairs gain = {};
             if (NORM && here) {
+                float ga[4], gb[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     ga[i] = __ldcg(t.gain + (HALVES ? at0 + i : at0 + 2 * i));
                     gb[i] = __ldcg(t.gain + (HALVES ? at1 + i : at0 + 2 * i + 1));
                 }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    gain.a[i] = pair_of(ga[2 * i], ga[2 * i + 1]);
+                    gain.b[i] = pair_of(gb[2 * i], gb[2 * i + 1]);
+                }
             }
-            const char* in = t.in + b * t.in_b + (long long)h0 * t.in_h + (long long)n0 * t.in_n;
-            const char* grad = GRADS ? t.grad + b * t.grad_b + (long long)h0 * t.grad_h + (long long)n0 * t.grad_n : nullptr;
-            char* out = t.out + b * t.out_b + (long long)h0 * t.out_h + (long long)n0 * t.out_n;
-            float lo[AHEAD][4], hi[AHEAD][4], dlo[GRADS ? AHEAD : 1][4], dhi[GRADS ? AHEAD : 1][4];
-            for (int first = warp * RPW + r0; first - r0 < rows; first += AHEAD * WARPS * RPW) {
+            // z.a = x.a fc.a + x.b fs.b, z.b = x.a fs.a + x.b fc.b; forward with the gains as factors
+            Pairs fc = cs, fs = sn;
+            if (NORM && !BACK) {
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const int row = first + u * WARPS * RPW, h = row >> p.log_tokens, n = row & ((1 << p.log_tokens) - 1);
+                for (int i = 0; i < 2; ++i) {
+                    fc.a[i] = mul2(cs.a[i], gain.a[i]);
+                    fc.b[i] = mul2(cs.b[i], gain.b[i]);
+                    fs.a[i] = mul2(sn.a[i], gain.a[i]);
+                    fs.b[i] = mul2(sn.b[i], gain.b[i]);
+                }
+            }
+            auto turned = [&](const Pairs& x) {
+                Pairs z;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        lo[u][i] = hi[u][i] = 0.f;
-                        if (GRADS) dlo[GRADS ? u : 0][i] = dhi[GRADS ? u : 0][i] = 0.f;
+                for (int i = 0; i < 2; ++i) {
+                    z.a[i] = fma2(x.a[i], fc.a[i], mul2(x.b[i], fs.b[i]));
+                    z.b[i] = fma2(x.a[i], fs.a[i], mul2(x.b[i], fc.b[i]));
+                }
+                return z;
+            };
+            int left = live ? heads[w] - head0 : 0;      // as `coming`, of the rows to be written
+            char* out = t.out + b * t.out_b + (long long)(first_head[w] + head0) * t.out_h + n * t.out_n;
+            const long long out_step = t.out_h * head_step;
+            // U rows at a time, whose chains of shuffles run beside one another
+            for (int s0 = 0; s0 < steps[w]; s0 += U) {
+                const int rows = min(U, steps[w] - s0);
+                asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - U) : "memory");
+                __syncwarp();
+                Raw<TYPE> x[U], d[GRADS ? U : 1];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {            // (of a row too many: what the place holds; nothing is done with it)
+                    const char* const from = ring_at + ((step + u) % DEPTH) * (STREAMS * STEP);
+                    x[u] = read_raw<TYPE, HALVES>(from, at0, at1);
+                    if constexpr (GRADS) d[u] = read_raw<TYPE, HALVES>(from + STEP, at0, at1);
+                }
+                __syncwarp();                            // all lanes have read: the places can be filled again
+                step += rows;
+                for (int u = 0; u < rows; ++u) issue();
+                Pairs z[U];
+                if constexpr (!GRADS) {
+                    float ss[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const Pairs v = widen<TYPE, HALVES>(x[u]);
+                        if constexpr (NORM) ss[u] = dot8(v, v);
+                        z[u] = turned(v);
                     }
-                    if (row < rows && n < tokens && here) {
-                        const char* x = in + h * t.in_h + n * t.in_n;
-                        load4<TYPE>(x + at0 * SIZE, lo[u]);
-                        load4<TYPE>(x + at1 * SIZE, hi[u]);
-                        if constexpr (GRADS) {
-                            const char* d = grad + h * t.grad_h + n * t.grad_n;
-                            load4<TYPE>(d + at0 * SIZE, dlo[u]);
-                            load4<TYPE>(d + at1 * SIZE, dhi[u]);
+                    if constexpr (NORM) {
+#pragma unroll
+                        for (int o = 1; o < LPR; o <<= 1)
+#pragma unroll
+                            for (int u = 0; u < U; ++u) ss[u] += __shfl_xor_sync(0xffffffffu, ss[u], o);
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            const uint64_t r = twice(rsqrtf(ss[u] * p.inv_D + p.eps));
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                z[u].a[i] = mul2(z[u].a[i], r);
+                                z[u].b[i] = mul2(z[u].b[i], r);
+                            }
                         }
+                    }
+                } else {
+                    static_assert(!GRADS || U == 1, "a row too many would count");
+                    const Pairs v = widen<TYPE, HALVES>(x[0]), y = turned(widen<TYPE, HALVES>(d[0]));     // y: gradient of the normed row
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        z[0].a[i] = mul2(y.a[i], gain.a[i]);
+                        z[0].b[i] = mul2(y.b[i], gain.b[i]);
+                    }
+                    float ss = dot8(v, v), dot = dot8(z[0], v);
+#pragma unroll
+                    for (int o = 1; o < LPR; o <<= 1) {
+                        ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                    }
+                    const float r1 = rsqrtf(ss * p.inv_D + p.eps);
+                    const uint64_t r = twice(r1), m = twice(-dot * r1 * r1 * p.inv_D);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        acc[w].a[i] = fma2(y.a[i], mul2(v.a[i], r), acc[w].a[i]);
+                        acc[w].b[i] = fma2(y.b[i], mul2(v.b[i], r), acc[w].b[i]);
+                        z[0].a[i] = mul2(r, fma2(m, v.a[i], z[0].a[i]));
+                        z[0].b[i] = mul2(r, fma2(m, v.b[i], z[0].b[i]));
                     }
                 }
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const int row = first + u * WARPS * RPW, h = row >> p.log_tokens, n = row & ((1 << p.log_tokens) - 1);
-                    if (row - r0 >= rows) break;        // the same for the whole warp
-                    float xa[4], xb[4], za[4], zb[4];
-                    auto pairs_of = [&](const float (&l)[4], const float (&m)[4], float (&a)[4], float (&bb)[4]) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            a[i] = HALVES ? l[i] : i < 2 ? l[2 * i] : m[2 * i - 4];
-                            bb[i] = HALVES ? m[i] : i < 2 ? l[2 * i + 1] : m[2 * i - 3];
-                        }
-                    };
-                    pairs_of(lo[u], hi[u], xa, xb);
-                    const int tt = min(n, tokens - 1);  // lanes without a row read some token's
-                    const float4 co = table[(tt * 2) * LPR + c], si = table[(tt * 2 + 1) * LPR + c];
-                    const float cs[4] = {co.x, co.y, co.z, co.w}, sn[4] = {si.x, si.y, si.z, si.w};
-                    if constexpr (!GRADS) {
-                        float r = 1.f;
-                        if constexpr (NORM) {
-                            float ss = 0.f;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) ss = fmaf(xa[i], xa[i], fmaf(xb[i], xb[i], ss));
-#pragma unroll
-                            for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                            r = rsqrtf(ss / (float)D + p.eps);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float a = NORM ? xa[i] * r * ga[i] : xa[i], bb = NORM ? xb[i] * r * gb[i] : xb[i];
-                            za[i] = fmaf(a, cs[i], -(bb * sn[i]));
-                            zb[i] = fmaf(a, sn[i], bb * cs[i]);
-                        }
-                    } else {
-                        float da[4], db[4], ss = 0.f, dot = 0.f;
-                        pairs_of(dlo[u], dhi[u], da, db);
-                        float ya[4], yb[4];             // gradient of the normed row
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            ya[i] = fmaf(da[i], cs[i], -(db[i] * sn[i]));
-                            yb[i] = fmaf(da[i], sn[i], db[i] * cs[i]);
-                            ss = fmaf(xa[i], xa[i], fmaf(xb[i], xb[i], ss));
-                            za[i] = ya[i] * ga[i];
-                            zb[i] = yb[i] * gb[i];
-                            dot = fmaf(za[i], xa[i], fmaf(zb[i], xb[i], dot));
-                        }
-                        if (!here) dot = 0.f;           // (gains of lanes without channels are not loaded)
-#pragma unroll
-                        for (int o = 1; o < LPR; o <<= 1) {
-                            ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                            dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                        }
-                        const float r = rsqrtf(ss / (float)D + p.eps), m = dot * r * r / (float)D;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            acc[w][i] = fmaf(ya[i], xa[i] * r, acc[w][i]);
-                            acc[w][4 + i] = fmaf(yb[i], xb[i] * r, acc[w][4 + i]);
-                            za[i] = r * fmaf(-m, xa[i], za[i]);
-                            zb[i] = r * fmaf(-m, xb[i], zb[i]);
-                        }
-                    }
-                    if (row < rows && n < tokens && here) {
-                        char* z = out + h * t.out_h + n * t.out_n;
-                        if (HALVES) {
-                            store4<TYPE>(z + at0 * SIZE, za[0], za[1], za[2], za[3]);
-                            store4<TYPE>(z + at1 * SIZE, zb[0], zb[1], zb[2], zb[3]);
-                        } else {
-                            store4<TYPE>(z + at0 * SIZE, za[0], zb[0], za[1], zb[1]);
-                            store4<TYPE>(z + at1 * SIZE, za[2], zb[2], za[3], zb[3]);
-                        }
-                    }
+                for (int u = 0; u < U; ++u) {
+                    if (left > 0) store_pairs<TYPE, HALVES>(out, at0, at1, z[u]);
+                    left -= head_step;
+                    out += out_step;
                 }
             }
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
     }
     grid_dependency_launch();
     if constexpr (GRADS) {
-        // the lanes' sums of the thread block, in a fixed order: rows of a warp, then warps
+        // the lanes' sums of the thread block, in a fixed order: rows of a warp, then warps; through the ring's memory
+        static_assert(sizeof(float) * WARPS * 2 * MAX_D <= ring_bytes(TYPE, true), "the sums fit the ring");
+        float (*sums)[2 * MAX_D] = reinterpret_cast<float (*)[2 * MAX_D]>(ring);
+        __syncthreads();
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float s = acc[w][e];
+                const float2 v = of_pair(e < 4 ? acc[w].a[e >> 1 & 1] : acc[w].b[e >> 1 & 1]);
+                float s = e & 1 ? v.y : v.x;
 #pragma unroll
                 for (int o = LPR; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
                 const int i = e & 3, channel = HALVES ? (e < 4 ? at0 : at1) + i : at0 + 2 * i + (e >> 2);
-                if (r0 == 0 && here) sums[warp][w * D + channel] = s;
+                if (lane < LPR && here) sums[warp][w * D + channel] = s;
             }
         __syncthreads();
         float* to = p.partial + ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * D;
@@ -376,17 +507,19 @@ int run_rotary(const rapid3_heads* s, const rapid3_rows* const (&in)[2], const r
     t.amplitude = turn->amplitude;
     for (int x = 0, end = 0; x < turn->axes; ++x) t.axis_end[x] = end += turn->axis_pairs[x];
     a.eps = eps;
+    a.inv_D = 1.f / (float)s->D;
     a.N = s->N;
     a.D = s->D;
-    while ((1 << a.log_tokens) < std::min(s->N, TOKENS)) ++a.log_tokens;
+    int lanes = 4;
+    while (8 * lanes < s->D) lanes *= 2;
+    const int slots = WARPS * (32 / lanes);
+    while ((1 << a.log_tokens) < std::min(s->N, slots)) ++a.log_tokens;
     const int tokens = 1 << a.log_tokens;
     a.tiles = (s->N + tokens - 1) / tokens;
     a.n_tiles = s->B * a.tiles;
     a.partial = static_cast<float*>(workspace);
-    int lanes = 4;
-    while (8 * lanes < s->D) lanes *= 2;
     // Where the tiles leave SMs without work their heads are shared out, down to one pass of a thread block's warps.
-    const int heads = s->H_q + s->H_k, pass = std::max(1, WARPS * (32 / lanes) / tokens);
+    const int heads = s->H_q + s->H_k, pass = slots / tokens;
     int groups = std::min((heads + pass - 1) / pass, std::max(1, 2 * SM_COUNT / a.n_tiles));
     a.heads_per_block = (heads + groups - 1) / groups;
     groups = (heads + a.heads_per_block - 1) / a.heads_per_block;
@@ -396,7 +529,7 @@ int run_rotary(const rapid3_heads* s, const rapid3_rows* const (&in)[2], const r
                         : s->type == RAPID3_F16 ? pick_lanes<RAPID3_F16>(lanes, halves, norm, back)
                                                 : pick_lanes<RAPID3_F32>(lanes, halves, norm, back);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (launch_kernel(kernel, dim3(blocks, groups), dim3(32 * WARPS), (size_t)tokens * 2 * lanes * sizeof(float4), st, a) != cudaSuccess)
+    if (launch_kernel(kernel, dim3(blocks, groups), dim3(32 * WARPS), ring_bytes(s->type, grads), st, a) != cudaSuccess)
         return RAPID3_ERR_CUDA;
     if (grads && launch_kernel(gain_kernel, dim3((2 * s->D + 31) / 32), dim3(1024), 0, st, (const float*)a.partial, blocks * groups, s->D, dq_gain,
                                dk_gain) != cudaSuccess)
