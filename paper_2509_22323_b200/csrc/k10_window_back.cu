@@ -14,11 +14,12 @@
 // products run beside the last one's results on their way out.  Tiles of first tokens see every row, far more than the others: where they
 // alone would keep a few SMs busy their blocks are shared out to several units, whose 32-bit results add_parts_kernel adds up.
 //
-// Roles (640 threads): warps 0-15 the element work, eight warps per score buffer (blocks go to the two buffers by turns): a warp owns 16
+// Roles (640 threads): warps 0-15 the element work, eight warps a block (the blocks go to the two sets of eight by turns): a warp owns 16
 // rows of the tile, a thread a quarter of two rows; warp 16 the producer (TMA; rows behind a sequence's last, which are not the caller's to
-// keep finite, are set to zero); warp 17 the UMMA issue: S and dP of block n + 1 go out before the second products of block n; warp 18 the
-// next unit.
-// TMEM: 0 and D: the accumulators; 256 + 64 (n & 1): S; 384 + 64 (n & 1): dP.
+// keep finite, are set to zero); warp 17 the UMMA issue: S and dP of block n + NBUF - 1 go out before the second products of block n; warp 18
+// the next unit.
+// TMEM: 0 and D: the accumulators; behind them NBUF buffers of 64 columns of S and 64 of dP.  Two at D = 128, where the columns end; at D = 64
+// three, with which a set finds its next block's S and dP there when it is through with one.
 // Every mbarrier wait is bounded, as in K8.
 #include <math.h>
 #include <stddef.h>
@@ -36,7 +37,7 @@ namespace {
 
 constexpr int WARPS = 16, PRODUCER_WARP = 16, MMA_WARP = 17, NEXT_WARP = 18, NTHREADS = 32 * (WARPS + 4);
 constexpr int ELEMENT_REGS = 104, LIGHT_REGS = 64;       // registers a thread of the element warps, of the others: of 640 x 96
-constexpr int TMEM_COLS = 512, S_COL = 256, DP_COL = 384;
+constexpr int TMEM_COLS = 512;
 constexpr int BLK_BYTES = 8192, XHALF_BYTES = 16384;
 constexpr int TAKE_AHEAD = 4, UNIT_USERS = WARPS + 2;
 constexpr int MAX_PARTS = 16, MAX_SLOTS = 2 * SM_COUNT;  // units of a shared-out tile; of all of them
@@ -64,6 +65,8 @@ struct Cfg {
     static constexpr int DH = D / 64;
     static constexpr int XTILE_BYTES = 128 * D * 2, Y_BYTES = 64 * D * 2;
     static constexpr int STAT_BYTES = 512;               // key unit: nlse and ndelta of the block's 64 rows
+    static constexpr int NBUF = D == 128 ? 2 : 3;
+    static constexpr int S_COL = 2 * D, BUF_COLS = 128;                 // dP 64 columns behind S
     static constexpr int STAGES = D == 128 ? 4 : 6;
     static constexpr int STAGE_BYTES = 2 * Y_BYTES;
     static constexpr int DATA_BYTES = 2 * XTILE_BYTES + STAGES * (STAGE_BYTES + STAT_BYTES);
@@ -88,7 +91,7 @@ struct Unit {
 struct __align__(16) Ctl {
     uint4 taken;
     unsigned long long taken_full, near_end, unit_full[2], unit_empty[2];
-    unsigned long long x_full, x_empty, tail_full, full[MAX_STAGES], empty[MAX_STAGES], t_full[2], p_full[2], done, drained, drain;
+    unsigned long long x_full, x_empty, tail_full, full[MAX_STAGES], empty[MAX_STAGES], t_full[3], p_full[3], done, drained, drain;
     uint32_t tmem_base;
     volatile int abort_flag;
     Unit unit[2];
@@ -221,7 +224,7 @@ __global__ void __launch_bounds__(NTHREADS, 1)
 window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                    const __grid_constant__ CUtensorMap td, const __grid_constant__ Params prm, int B) {
     using C = Cfg<D>;
-    constexpr int DH = C::DH, STAGES = C::STAGES;
+    constexpr int DH = C::DH, STAGES = C::STAGES, NBUF = C::NBUF;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), pad = ((raw + 1023u) & ~1023u) - raw;
     uint8_t* smem = smem_raw + pad;
@@ -241,7 +244,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
         for (uint32_t x = lane; x < bars; x += 32) {
             uint32_t count = 1;
             if (has(x, offsetof(Ctl, unit_empty), 2)) count = UNIT_USERS;
-            if (has(x, offsetof(Ctl, p_full), 2)) count = 8;                   // one arrival per warp of the buffer
+            if (has(x, offsetof(Ctl, p_full), 3)) count = 8;                   // one arrival per warp of the buffer
             if (has(x, offsetof(Ctl, drained), 1)) count = WARPS;
             mbar_init(smem_u32(ctl) + 8 * (at + x), count);
         }
@@ -408,19 +411,20 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                     for (int w = 0; w < 2; ++w)
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks)
-                            mma_ss(tmem_base + (w ? DP_COL : S_COL) + 64 * (M & 1),
+                            mma_ss(tmem_base + C::S_COL + C::BUF_COLS * (M % NBUF) + 64 * w,
                                    smem_desc_sw128(sX + w * C::XTILE_BYTES + (ks / 4) * XHALF_BYTES + (ks % 4) * 32, 16, 1024),
                                    smem_desc_sw128(y + w * C::Y_BYTES + (ks / 4) * BLK_BYTES + (ks % 4) * 32, 16, 1024), idesc1, ks > 0);
-                    tc_commit(bT + 8 * (M & 1));
+                    tc_commit(bT + 8 * (M % NBUF));
                     if (j == n - 1) tc_commit(bXE);
                     return true;
                 };
-                if (n > 0) ok = wait(bX, n_x & 1) && first_products(0);
+                if (n > 0) ok = wait(bX, n_x & 1);
+                for (int j = 0; ok && j < min(n, NBUF - 1); ++j) ok = first_products(j);
                 for (int j = 0; ok && j < n; ++j) {
-                    // S and dP of block j + 1 take the buffers of block j - 1, whose second products were issued before
-                    if (j + 1 < n && !(ok = first_products(j + 1))) break;
+                    // S and dP of block j + NBUF - 1 take the buffers of block j - 1, whose second products were issued before
+                    if (j + NBUF - 1 < n && !(ok = first_products(j + NBUF - 1))) break;
                     const uint32_t M = N + j, s = M % STAGES;
-                    if (!(ok = wait(bP + 8 * (M & 1), (M >> 1) & 1))) break;
+                    if (!(ok = wait(bP + 8 * (M % NBUF), (M / NBUF) & 1))) break;
                     // the first of a unit's second products overwrite the accumulators: those of the unit before have been read
                     if (j == 0 && n_x > 0 && !(ok = wait(bDE, (n_x - 1) & 1))) break;
                     tc_fence_after();
@@ -431,7 +435,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                         if (w == 0 || key)
 #pragma unroll
                             for (int ks = 0; ks < 4; ++ks)
-                                mma_ts(tmem_base + w * D, tmem_base + (w ? S_COL : DP_COL) + 64 * (M & 1) + ks * 8,
+                                mma_ts(tmem_base + w * D, tmem_base + C::S_COL + C::BUF_COLS * (M % NBUF) + (w ? 0 : 64) + ks * 8,
                                        smem_desc_sw128(y + w * C::Y_BYTES + ks * 2048, BLK_BYTES, 1024), idesc2, (j > 0 || ks > 0) ? 1u : 0u);
                     tc_commit(bE + 8 * s);
                 }
@@ -449,7 +453,6 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
         reg_inc<ELEMENT_REGS>();
         const int set = warp >> 3, group = 2 * (warp & 3) + ((warp >> 2) & 1), cg = lane & 3;
         const uint32_t lane_addr = tmem_base + ((uint32_t)(16 * group) << 16);
-        const uint32_t tS = lane_addr + S_COL + 64 * set, tP = lane_addr + DP_COL + 64 * set;
         const float c2 = prm.scale_log2;
         uint32_t N = 0, n_x = 0;
         for (uint32_t i = 0;; ++i) {
@@ -481,7 +484,8 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                     const int3 reach = u.reach[group];
                     const bool act = (col0 < reach.y && col0 + 64 > reach.x) || col0 < reach.z;
                     const bool compare = !((col0 >= whole.x && col0 + 64 <= whole.y) || (col0 >= whole.z && col0 + 64 <= whole.w));
-                    wait(bT + 8 * set, (M >> 1) & 1);
+                    const uint32_t buf = M % NBUF, tS = lane_addr + C::S_COL + C::BUF_COLS * buf, tP = tS + 64;
+                    wait(bT + 8 * buf, (M / NBUF) & 1);
                     if (KEY) wait(bF + 8 * (M % STAGES), (M / STAGES) & 1);    // nlse and ndelta of the block, read below
                     if (__any_sync(0xffffffffu, ctl->abort_flag)) return;
                     tc_fence_after();
@@ -561,7 +565,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                     tc_wait_st();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bP + 8 * set);
+                    if (lane == 0) mbar_arrive(bP + 8 * buf);
                 }
             };
             const bool key = u.key;
