@@ -14,12 +14,19 @@
 // products run beside the last one's results on their way out.  Tiles of first tokens see every row, far more than the others: where they
 // alone would keep a few SMs busy their blocks are shared out to several units, whose 32-bit results add_parts_kernel adds up.
 //
-// Roles (640 threads): warps 0-15 the element work, eight warps a block (the blocks go to the two sets of eight by turns): a warp owns 16
-// rows of the tile, a thread a quarter of two rows; warp 16 the producer (TMA; rows behind a sequence's last, which are not the caller's to
-// keep finite, are set to zero); warp 17 the UMMA issue: S and dP of block n + NBUF - 1 go out before the second products of block n; warp 18
-// the next unit.
-// TMEM: 0 and D: the accumulators; behind them NBUF buffers of 64 columns of S and 64 of dP.  Two at D = 128, where the columns end; at D = 64
-// three, with which a set finds its next block's S and dP there when it is through with one.
+// Roles (640 threads): warps 0-15 the element work: a warp owns 16 rows of the tile, a thread a quarter of two rows; warp 16 the producer
+// (TMA; rows behind a sequence's last, which are not the caller's to keep finite, are set to zero); warp 17 the UMMA issue; warp 18 the next unit.
+//
+// D = 64: eight warps a block, the blocks go to the two sets of eight by turns.  S and dP of block n + 2 go out before the second products of
+// block n; tensor memory holds three buffers of 64 columns of S and 64 of dP behind the accumulators.
+// D = 128: the first products are what bounds the kernel, not by the tensor cores' rate but by the shared memory that feeds them: with 64
+// columns 16 x (128 + 64) numbers are read for 16 x 128 x 64 products, 48 cycles of the memory's 128 bytes for 32 cycles of work (measured: 63).
+// So the blocks are 128 rows wide and the warps' two sets take their halves.  Tensor memory then holds one S and one dP beside the accumulators
+// (0: dK or dQ, 128: dV, 256: S, 384: dP), and the element work goes in two steps: P from S, which stays in registers, so that the next
+// block's S can follow at once; then dS from dP, and both, rounded, over the dP that the warp has read.  What is left in one chain is dS, the
+// second products and the next block's dP (2000 cycles of a block's 3300); the element work takes as long, 350 instructions a warp at one in
+// nine cycles.  Training pass of 4095 causal tokens, 32 heads on 8, window of 1024: blocks of 64 355 us, of 128 with P over S 349, so 335.  The exponential
+// unit is not what it waits for: with a quarter or half of the powers on the fma units it took 340 to 343 us.
 // Every mbarrier wait is bounded, as in K8.
 #include <math.h>
 #include <stddef.h>
@@ -39,7 +46,7 @@ constexpr int WARPS = 16, PRODUCER_WARP = 16, MMA_WARP = 17, NEXT_WARP = 18, NTH
 constexpr int ELEMENT_REGS = 104, LIGHT_REGS = 64;       // registers a thread of the element warps, of the others: of 640 x 96
 constexpr int TMEM_COLS = 512;
 constexpr int BLK_BYTES = 8192, XHALF_BYTES = 16384;
-constexpr int TAKE_AHEAD = 4, UNIT_USERS = WARPS + 2;
+constexpr int TAKE_AHEAD = 4, UNIT_USERS = WARPS + 2, ABORT_EVERY = 32;
 constexpr int MAX_PARTS = 16, MAX_SLOTS = 2 * SM_COUNT;  // units of a shared-out tile; of all of them
 
 __device__ int status_word;
@@ -50,7 +57,7 @@ struct Params {
     const float* nlse;           // [B][H][padded]: minus log sum exp in base 2; -inf: a row that has no P
     const float* ndelta;         // minus delta
     float* partial;              // [slot][128][2 D]
-    int padded;                  // query rows of a head in these, a multiple of 64
+    int padded;                  // query rows of a head in these, a multiple of 128
     int H, H_kv, group;
     int key_tiles, row_tiles;    // of a head
     int sink_tiles, parts;       // the first key tiles, and how many units share one
@@ -63,11 +70,13 @@ struct Params {
 template <int D>
 struct Cfg {
     static constexpr int DH = D / 64;
-    static constexpr int XTILE_BYTES = 128 * D * 2, Y_BYTES = 64 * D * 2;
-    static constexpr int STAT_BYTES = 512;               // key unit: nlse and ndelta of the block's 64 rows
-    static constexpr int NBUF = D == 128 ? 2 : 3;
-    static constexpr int S_COL = 2 * D, BUF_COLS = 128;                 // dP 64 columns behind S
-    static constexpr int STAGES = D == 128 ? 4 : 6;
+    static constexpr bool WIDE = D == 128;
+    static constexpr int WIDTH = WIDE ? 128 : 64;        // rows of a block
+    static constexpr int XTILE_BYTES = 128 * D * 2, Y_BYTES = WIDTH * D * 2, YHALF_BYTES = WIDTH * 128;     // (a half: 64 channels)
+    static constexpr int STAT_BYTES = 8 * WIDTH;         // key unit: nlse and ndelta of the block's rows
+    static constexpr int NBUF = 3;
+    static constexpr int S_COL = 2 * D, BUF_COLS = 128;                 // dP 64 columns behind S (WIDE: 128)
+    static constexpr int STAGES = WIDE ? 2 : 6;
     static constexpr int STAGE_BYTES = 2 * Y_BYTES;
     static constexpr int DATA_BYTES = 2 * XTILE_BYTES + STAGES * (STAGE_BYTES + STAT_BYTES);
 };
@@ -86,6 +95,7 @@ struct Unit {
     // below z.
     int4 whole[8];
     int3 reach[8];
+    int2 free[WARPS];            // of an element warp: the entries of a head's list whose 64 columns all rows see, from where and how many
 };
 
 struct __align__(16) Ctl {
@@ -165,7 +175,22 @@ __device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int grou
     }
 }
 
-__device__ __forceinline__ Unit unit_of(const Params& p, int B, int L) {
+// Unit::free, from the first of the two ranges.
+__device__ __forceinline__ int2 free_of(const Unit& u, const int4& whole, int set, bool wide) {
+    const int shift = wide ? 7 : 6, add = wide ? 64 * set : 0, from = max((whole.x - add + (1 << shift) - 1) >> shift, u.blocks.from);
+    const int to = min(((whole.y - add - 64) >> shift) + 1, u.blocks.to), gap = u.blocks.from - u.blocks.first;
+    return make_int2(from - gap, max(to - from, 0));
+}
+// Blocks of 64 as blocks of 128.
+__device__ __forceinline__ Blocks doubled(const Blocks& b) {
+    Blocks r;
+    r.from = b.from >> 1;
+    r.to = (b.to + 1) >> 1;
+    r.first = min((b.first + 1) >> 1, r.from);
+    return r;
+}
+
+__device__ __forceinline__ Unit unit_of(const Params& p, int B, int L, bool wide) {
     Unit u;
     u.key = L < p.key_units;
     u.slot = -1;
@@ -197,6 +222,7 @@ __device__ __forceinline__ Unit unit_of(const Params& p, int B, int L) {
     const int last = min(u.first + 128, u.end);
     u.blocks = u.first >= last ? Blocks{0, 0, 0} : u.key ? query_blocks(p.w, u.first, last, u.rows, u.keys)
                                                          : key_blocks(p.w, u.first, last, u.rows, u.keys);
+    if (wide && u.blocks.count() > 0) u.blocks = doubled(u.blocks);
     u.per_head = u.blocks.count();
     const int n = u.key ? p.group * u.per_head : u.per_head;
     u.begin = (int)((long long)n * part / parts);
@@ -224,7 +250,8 @@ __global__ void __launch_bounds__(NTHREADS, 1)
 window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                    const __grid_constant__ CUtensorMap td, const __grid_constant__ Params prm, int B) {
     using C = Cfg<D>;
-    constexpr int DH = C::DH, STAGES = C::STAGES, NBUF = C::NBUF;
+    constexpr int DH = C::DH, STAGES = C::STAGES, NBUF = C::NBUF, WIDTH = C::WIDTH;
+    constexpr bool WIDE = C::WIDE;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), pad = ((raw + 1023u) & ~1023u) - raw;
     uint8_t* smem = smem_raw + pad;
@@ -244,7 +271,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
         for (uint32_t x = lane; x < bars; x += 32) {
             uint32_t count = 1;
             if (has(x, offsetof(Ctl, unit_empty), 2)) count = UNIT_USERS;
-            if (has(x, offsetof(Ctl, p_full), 3)) count = 8;                   // one arrival per warp of the buffer
+            if (has(x, offsetof(Ctl, p_full), 3)) count = WIDE ? WARPS : 8;     // one arrival per warp that works on the buffer
             if (has(x, offsetof(Ctl, drained), 1)) count = WARPS;
             mbar_init(smem_u32(ctl) + 8 * (at + x), count);
         }
@@ -285,13 +312,15 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
             if (i > 1 && !wait_lane0(bUE + 8 * (i & 1), ((i >> 1) & 1) ^ 1)) break;
             Unit& to = ctl->unit[i & 1];
             if (L >= 0) {
-                const Unit u = unit_of(prm, B, L);
+                const Unit u = unit_of(prm, B, L, C::WIDE);
                 if (lane < 8) {
                     int4 whole;
                     int3 reach;
                     bounds_of(prm.w, u, lane, whole, reach);
                     to.whole[lane] = whole;
                     to.reach[lane] = reach;
+#pragma unroll
+                    for (int set = 0; set < 2; ++set) to.free[2 * lane + set] = free_of(u, whole, set, C::WIDE);
                 }
                 if (lane == 0) {
                     to.n = u.n; to.key = u.key; to.b = u.b; to.h = u.h;
@@ -329,7 +358,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
             const Blocks blocks = u.blocks;
             const CUtensorMap* const x1 = key ? &tk : &tq, * const x2 = key ? &tv : &td, * const y1 = key ? &tq : &tk, * const y2 = key ? &td : &tv;
             const int y_len = key ? u.rows : u.keys, y_places = key ? prm.w.n_q : prm.w.n_kv;
-            const int tail = y_len < y_places && (y_len & 63) ? y_len >> 6 : -1;
+            const int tail = y_len < y_places && y_len % WIDTH ? y_len / WIDTH : -1;
             if (n == 0 && lane == 0) mbar_arrive(bNE);
             Walk at(u);
             for (int j = 0; j < n; ++j, ++N, at.next(per_head)) {
@@ -351,37 +380,47 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                 }
                 const uint32_t s = N % STAGES;
                 const int block = blocks.at(at.j), yh = key ? h * prm.group + at.head : h / prm.group;
-                if (!(ok = wait_lane0(bE + 8 * s, ((N / STAGES) & 1) ^ 1))) break;
-                const uint32_t y = sY + s * C::STAGE_BYTES;
-                const bool mend = block == tail;
-                if (lane == 0) {
-                    const uint32_t bar = mend ? bTail : bF + 8 * s;
-                    mbar_arrive_expect_tx(bar, C::STAGE_BYTES + (key ? C::STAT_BYTES : 0));
+                // WIDE: Y1 and Y2 have stages and barriers of their own
+                constexpr int LOADS = WIDE ? 2 : 1;
 #pragma unroll
-                    for (int dh = 0; dh < DH; ++dh) {
-                        tma_load_4d(y + dh * BLK_BYTES, y1, bar, dh * 64, block * 64, yh, b);
-                        tma_load_4d(y + C::Y_BYTES + dh * BLK_BYTES, y2, bar, dh * 64, block * 64, yh, b);
-                    }
-                    if (key) {
-                        const long long from = ((long long)b * prm.H + yh) * prm.padded + block * 64;
-                        const uint32_t to = smem_u32(stats) + s * C::STAT_BYTES;
-                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
-                                     ::"r"(to), "l"(prm.nlse + from), "r"(bar) : "memory");
-                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
-                                     ::"r"(to + 256), "l"(prm.ndelta + from), "r"(bar) : "memory");
-                    }
-                }
-                __syncwarp();
-                if (mend) {
-                    if (!(ok = wait_lane0(bTail, n_tail++ & 1))) break;
-                    uint8_t* to = smem + (y - sX);       // a row of a half is 128 bytes; the swizzle moves bytes within it
-                    for (int z = (y_len & 63) * 8 + lane; z < 64 * 8; z += 32)
+                for (int x = 0; x < LOADS; ++x) {
+                    if (!(ok = wait_lane0(bE + 8 * (x * STAGES + s), ((N / STAGES) & 1) ^ 1))) break;
+                    const uint32_t y = sY + s * C::STAGE_BYTES;
+                    const bool mend = block == tail;
+                    const uint32_t full = bF + 8 * (x * STAGES + s);
+                    if (lane == 0) {
+                        const uint32_t bar = mend ? bTail : full;
+                        mbar_arrive_expect_tx(bar, C::STAGE_BYTES / LOADS + (key && x == 0 ? C::STAT_BYTES : 0));
 #pragma unroll
-                        for (int dh = 0; dh < 2 * DH; ++dh) *reinterpret_cast<uint4*>(to + dh * BLK_BYTES + 16 * z) = make_uint4(0, 0, 0, 0);
-                    fence_proxy_async_smem();
+                        for (int dh = 0; dh < DH; ++dh)
+#pragma unroll
+                            for (int a = 0; a < WIDTH / 64; ++a) {
+                                const int row = block * WIDTH + 64 * a;
+                                if (!WIDE || x == 0) tma_load_4d(y + dh * C::YHALF_BYTES + a * BLK_BYTES, y1, bar, dh * 64, row, yh, b);
+                                if (!WIDE || x == 1) tma_load_4d(y + C::Y_BYTES + dh * C::YHALF_BYTES + a * BLK_BYTES, y2, bar, dh * 64, row, yh, b);
+                            }
+                        if (key && x == 0) {             // (with Y1, whose stage stays until dS is there)
+                            const long long from = ((long long)b * prm.H + yh) * prm.padded + block * WIDTH;
+                            const uint32_t to = smem_u32(stats) + s * C::STAT_BYTES;
+                            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %3, [%2];"
+                                             ::"r"(to), "l"(prm.nlse + from), "r"(bar), "n"(4 * WIDTH) : "memory");
+                            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %3, [%2];"
+                                             ::"r"(to + 4 * WIDTH), "l"(prm.ndelta + from), "r"(bar), "n"(4 * WIDTH) : "memory");
+                        }
+                    }
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bF + 8 * s);
+                    if (mend) {
+                        if (!(ok = wait_lane0(bTail, n_tail++ & 1))) break;
+                        uint8_t* to = smem + (y - sX) + (x == 1 ? C::Y_BYTES : 0);       // a row of a half is 128 bytes; the swizzle moves bytes within it
+                        for (int z = y_len % WIDTH * 8 + lane; z < WIDTH * 8; z += 32)
+#pragma unroll
+                            for (int dh = 0; dh < 2 * DH / LOADS; ++dh) *reinterpret_cast<uint4*>(to + dh * C::YHALF_BYTES + 16 * z) = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(full);
+                    }
                 }
+                if (!ok) break;
             }
             if (!ok) break;
             if (lane == 0) mbar_arrive(bUE + 8 * (i & 1));
@@ -389,12 +428,15 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
         if (ctl->abort_flag && lane == 0) {              // no copy may land after the thread block has left
             if (n_x > 0) mbar_wait(bX, (n_x - 1) & 1, 1u << 20);
             if (n_tail > 0) mbar_wait(bTail, (n_tail - 1) & 1, 1u << 20);
-            for (uint32_t z = N > STAGES ? N - STAGES : 0; z < N; ++z) mbar_wait(bF + 8 * (z % STAGES), (z / STAGES) & 1, 1u << 20);
+            for (uint32_t z = N > STAGES ? N - STAGES : 0; z < N; ++z)
+                for (int x = 0; x < (WIDE ? 2 : 1); ++x) mbar_wait(bF + 8 * (x * STAGES + z % STAGES), (z / STAGES) & 1, 1u << 20);
+            // (of a block whose first load alone was issued)
+            if (WIDE) mbar_wait(bF + 8 * (N % STAGES), (N / STAGES) & 1, 1u << 12);
         }
         __syncwarp();
     } else if (warp == MMA_WARP) {
         if (elect_one()) {
-            constexpr uint32_t idesc1 = idesc16<TYPE>(128, 64, 0, 0), idesc2 = idesc16<TYPE>(128, D, 0, 1);
+            constexpr uint32_t idesc1 = idesc16<TYPE>(128, WIDTH, 0, 0), idesc2 = idesc16<TYPE>(128, D, 0, 1);
             uint32_t N = 0, n_x = 0;
             bool ok = true;
             for (uint32_t i = 0; ok; ++i) {
@@ -402,42 +444,82 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                 const int n = ctl->unit[i & 1].n;
                 const bool key = ctl->unit[i & 1].key;
                 if (n < 0) break;
-                auto first_products = [&](int j) -> bool {
-                    const uint32_t M = N + j, s = M % STAGES;
-                    if (!wait(bF + 8 * s, (M / STAGES) & 1)) return false;
-                    tc_fence_after();
-                    const uint32_t y = sY + s * C::STAGE_BYTES;
-#pragma unroll
-                    for (int w = 0; w < 2; ++w)
+                if constexpr (WIDE) {
+                    // w = 0: S from Y1, 1: dP from Y2
+                    auto first_product = [&](int j, int w) -> bool {
+                        const uint32_t M = N + j, s = M % STAGES;
+                        if (!wait(bF + 8 * (w * STAGES + s), (M / STAGES) & 1)) return false;
+                        tc_fence_after();
+                        const uint32_t y = sY + s * C::STAGE_BYTES + w * C::Y_BYTES;
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks)
-                            mma_ss(tmem_base + C::S_COL + C::BUF_COLS * (M % NBUF) + 64 * w,
-                                   smem_desc_sw128(sX + w * C::XTILE_BYTES + (ks / 4) * XHALF_BYTES + (ks % 4) * 32, 16, 1024),
-                                   smem_desc_sw128(y + w * C::Y_BYTES + (ks / 4) * BLK_BYTES + (ks % 4) * 32, 16, 1024), idesc1, ks > 0);
-                    tc_commit(bT + 8 * (M % NBUF));
-                    if (j == n - 1) tc_commit(bXE);
-                    return true;
-                };
-                if (n > 0) ok = wait(bX, n_x & 1);
-                for (int j = 0; ok && j < min(n, NBUF - 1); ++j) ok = first_products(j);
-                for (int j = 0; ok && j < n; ++j) {
-                    // S and dP of block j + NBUF - 1 take the buffers of block j - 1, whose second products were issued before
-                    if (j + NBUF - 1 < n && !(ok = first_products(j + NBUF - 1))) break;
-                    const uint32_t M = N + j, s = M % STAGES;
-                    if (!(ok = wait(bP + 8 * (M % NBUF), (M / NBUF) & 1))) break;
-                    // the first of a unit's second products overwrite the accumulators: those of the unit before have been read
-                    if (j == 0 && n_x > 0 && !(ok = wait(bDE, (n_x - 1) & 1))) break;
-                    tc_fence_after();
-                    const uint32_t y = sY + s * C::STAGE_BYTES;
-                    // key unit: dK += dS^T Q, dV += P^T dO; row unit: dQ += dS K
+                            mma_ss(tmem_base + C::S_COL + 128 * w, smem_desc_sw128(sX + w * C::XTILE_BYTES + (ks / 4) * XHALF_BYTES + (ks % 4) * 32, 16, 1024),
+                                   smem_desc_sw128(y + (ks / 4) * C::YHALF_BYTES + (ks % 4) * 32, 16, 1024), idesc1, ks > 0);
+                        tc_commit(bT + 8 * w);
+                        if (w == 1 && !key) tc_commit(bE + 8 * (STAGES + s));  // of a row unit V has no other product
+                        if (w == 1 && j == n - 1) tc_commit(bXE);
+                        return true;
+                    };
+                    // w = 0: += dS Y1, 1: dV += P Y2; every 32 columns of dP became 16 of P and 16 of dS
+                    auto second_product = [&](int j, int w) {
+                        const uint32_t s = (N + j) % STAGES, y = sY + s * C::STAGE_BYTES + w * C::Y_BYTES;
+                        tc_fence_after();
 #pragma unroll
-                    for (int w = 0; w < 2; ++w)
-                        if (w == 0 || key)
+                        for (int ks = 0; ks < 8; ++ks)
+                            mma_ts(tmem_base + w * D, tmem_base + C::S_COL + 128 + (w ? 0 : 16) + (ks / 2) * 32 + (ks % 2) * 8,
+                                   smem_desc_sw128(y + ks * 2048, C::YHALF_BYTES, 1024), idesc2, (j > 0 || ks > 0) ? 1u : 0u);
+                        tc_commit(bE + 8 * (w * STAGES + s));
+                    };
+                    if (n > 0) ok = wait(bX, n_x & 1) && first_product(0, 0) && first_product(0, 1);
+                    for (int j = 0; ok && j < n; ++j) {
+                        const uint32_t M = N + j;
+                        if (!(ok = wait(bP, M & 1))) break;                    // S has been read
+                        if (j + 1 < n && !(ok = first_product(j + 1, 0))) break;
+                        if (!(ok = wait(bP + 8, M & 1))) break;                // P and dS are there
+                        // the first of a unit's second products overwrite the accumulators: those of the unit before have been read
+                        if (j == 0 && n_x > 0 && !(ok = wait(bDE, (n_x - 1) & 1))) break;
+                        if (key) second_product(j, 1);
+                        second_product(j, 0);
+                        if (j + 1 < n && !(ok = first_product(j + 1, 1))) break;
+                    }
+                } else {
+                    auto first_products = [&](int j) -> bool {
+                        const uint32_t M = N + j, s = M % STAGES;
+                        if (!wait(bF + 8 * s, (M / STAGES) & 1)) return false;
+                        tc_fence_after();
+                        const uint32_t y = sY + s * C::STAGE_BYTES;
 #pragma unroll
-                            for (int ks = 0; ks < 4; ++ks)
-                                mma_ts(tmem_base + w * D, tmem_base + C::S_COL + C::BUF_COLS * (M % NBUF) + (w ? 0 : 64) + ks * 8,
-                                       smem_desc_sw128(y + w * C::Y_BYTES + ks * 2048, BLK_BYTES, 1024), idesc2, (j > 0 || ks > 0) ? 1u : 0u);
-                    tc_commit(bE + 8 * s);
+                        for (int w = 0; w < 2; ++w)
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks)
+                                mma_ss(tmem_base + C::S_COL + C::BUF_COLS * (M % NBUF) + 64 * w,
+                                       smem_desc_sw128(sX + w * C::XTILE_BYTES + (ks / 4) * XHALF_BYTES + (ks % 4) * 32, 16, 1024),
+                                       smem_desc_sw128(y + w * C::Y_BYTES + (ks / 4) * BLK_BYTES + (ks % 4) * 32, 16, 1024), idesc1, ks > 0);
+                        tc_commit(bT + 8 * (M % NBUF));
+                        if (j == n - 1) tc_commit(bXE);
+                        return true;
+                    };
+                    if (n > 0) ok = wait(bX, n_x & 1);
+                    for (int j = 0; ok && j < min(n, NBUF - 1); ++j) ok = first_products(j);
+                    for (int j = 0; ok && j < n; ++j) {
+                        // S and dP of block j + NBUF - 1 take the buffers of block j - 1, whose second products were issued before
+                        if (j + NBUF - 1 < n && !(ok = first_products(j + NBUF - 1))) break;
+                        const uint32_t M = N + j, s = M % STAGES;
+                        if (!(ok = wait(bP + 8 * (M % NBUF), (M / NBUF) & 1))) break;
+                        // the first of a unit's second products overwrite the accumulators: those of the unit before have been read
+                        if (j == 0 && n_x > 0 && !(ok = wait(bDE, (n_x - 1) & 1))) break;
+                        tc_fence_after();
+                        const uint32_t y = sY + s * C::STAGE_BYTES;
+                        // key unit: dK += dS^T Q, dV += P^T dO; row unit: dQ += dS K
+#pragma unroll
+                        for (int w = 0; w < 2; ++w)
+                            if (w == 0 || key)
+#pragma unroll
+                                for (int ks = 0; ks < 4; ++ks)
+                                    mma_ts(tmem_base + w * D, tmem_base + C::S_COL + C::BUF_COLS * (M % NBUF) + (w ? 0 : 64) + ks * 8,
+                                           smem_desc_sw128(y + w * C::Y_BYTES + ks * 2048, BLK_BYTES, 1024), idesc2, (j > 0 || ks > 0) ? 1u : 0u);
+                        tc_commit(bE + 8 * s);
+                    }
                 }
                 if (!ok) break;
                 if (n > 0) {
@@ -475,97 +557,188 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                         }
                 }
                 Walk at(u);
-                const int per_head = u.per_head;
-                for (int j = 0; j < n; ++j, at.next(per_head)) {
-                    const uint32_t M = N + j;
-                    if ((int)(M & 1) != set) continue;
-                    const int col0 = 64 * u.blocks.at(at.j);
-                    const int4 whole = u.whole[group];
-                    const int3 reach = u.reach[group];
-                    const bool act = (col0 < reach.y && col0 + 64 > reach.x) || col0 < reach.z;
-                    const bool compare = !((col0 >= whole.x && col0 + 64 <= whole.y) || (col0 >= whole.z && col0 + 64 <= whole.w));
-                    const uint32_t buf = M % NBUF, tS = lane_addr + C::S_COL + C::BUF_COLS * buf, tP = tS + 64;
-                    wait(bT + 8 * buf, (M / NBUF) & 1);
-                    if (KEY) wait(bF + 8 * (M % STAGES), (M / STAGES) & 1);    // nlse and ndelta of the block, read below
-                    if (__any_sync(0xffffffffu, ctl->abort_flag)) return;
-                    tc_fence_after();
-                    if (act) {
-                        uint32_t s[2][16], d[2][16];
+                const int per_head = u.per_head, free_from = u.free[2 * group + set].x;
+                const uint32_t free_count = u.free[2 * group + set].y;
+                // Scores of columns that the thread's two rows do not see become -inf: numbers 4 k + 2 e, + 1 of half x are columns 32 x + 8 k + 2 cg, + 1 of
+                // row e.
+                auto hide = [&](int col0, auto&& score) {
+                    const int row = u.first + 16 * group + (lane >> 2), off = u.keys - u.rows, end = u.end;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = row + 8 * e;
+                        uint32_t bits[2];
+                        if (KEY) {
+                            int lo, hi, full_lo, full_hi;
+                            rows_of_key(prm.w, r, u.rows, off, lo, hi);
+                            full_rows(prm.w, u.rows, off, full_lo, full_hi);
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const int c0 = col0 + 32 * x;
+                                bits[x] = (bits_below(hi - c0) & ~bits_below(lo - c0)) | (bits_below(full_hi - c0) & ~bits_below(full_lo - c0));
+                            }
+                        } else {
+                            prm.w.seen_bits(r + off, r < end ? u.keys : 0, col0, bits);
+                        }
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
-                            tmem_ld16x256_x4(tS + 32 * x, s[x]);
-                            tmem_ld16x256_x4(tP + 32 * x, d[x]);
+                            const uint32_t w = bits[x] >> (2 * cg);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                if (!(w >> (8 * k) & 1u)) score(x, 4 * k + 2 * e) = 0xff800000u;
+                                if (!(w >> (8 * k + 1) & 1u)) score(x, 4 * k + 2 * e + 1) = 0xff800000u;
+                            }
                         }
-                        tc_wait_ld();
-                        if (compare) {
-                            // the columns that the two rows see, as bits; the thread's 8 k + 2 cg + x at 8 k + x
-                            const int row = u.first + 16 * group + (lane >> 2), off = u.keys - u.rows, end = u.end;
+                    }
+                };
+                if constexpr (WIDE) {
+                    for (int j = 0; j < n; ++j, at.next(per_head)) {
+                        const uint32_t M = N + j, buf = M % STAGES;
+                        int col0 = 0;
+                        bool act = true, compare = false;
+                        if ((uint32_t)(at.j - free_from) >= free_count) {
+                            col0 = WIDTH * u.blocks.at(at.j) + 64 * set;
+                            const int4 whole = u.whole[group];
+                            const int3 reach = u.reach[group];
+                            act = (col0 < reach.y && col0 + 64 > reach.x) || col0 < reach.z;
+                            compare = !((col0 >= whole.x && col0 + 64 <= whole.y) || (col0 >= whole.z && col0 + 64 <= whole.w));
+                        }
+                        const uint32_t tS = lane_addr + C::S_COL + 64 * set, tP = tS + 128;
+                        const uint64_t* const st = reinterpret_cast<const uint64_t*>(stats + buf * C::STAT_BYTES + 256 * set) + cg;
+                        uint32_t s[32];
+                        // (nothing up to the end of the unit depends on a wait's result; the flag is looked at once in a while)
+                        if (j % ABORT_EVERY == 0 && __any_sync(0xffffffffu, ctl->abort_flag)) return;
+                        if (KEY) wait(bF + 8 * buf, (M / STAGES) & 1);             // nlse and ndelta, read below
+                        wait(bT, M & 1);
+                        __syncwarp();
+                        tc_fence_after();
+                        if (act) {
+                            tmem_ld16x256_x8(tS, s);
+                            tc_wait_ld();
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bP);
+                        if (act) {
+                            if (compare) hide(col0, [&](int x, int i) -> uint32_t& { return s[16 * x + i]; });
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int r = row + 8 * e;
-                                uint32_t bits[2];
-                                if (KEY) {
-                                    int lo, hi, full_lo, full_hi;
-                                    rows_of_key(prm.w, r, u.rows, off, lo, hi);
-                                    full_rows(prm.w, u.rows, off, full_lo, full_hi);
+                            for (int k = 0; k < 8; ++k) {
+                                uint64_t cl;
+                                if (KEY) cl = st[4 * k];
 #pragma unroll
-                                    for (int x = 0; x < 2; ++x) {
-                                        const int c0 = col0 + 32 * x;
-                                        bits[x] = (bits_below(hi - c0) & ~bits_below(lo - c0)) | (bits_below(full_hi - c0) & ~bits_below(full_lo - c0));
-                                    }
-                                } else {
-                                    prm.w.seen_bits(r + off, r < end ? u.keys : 0, col0, bits);
-                                }
-#pragma unroll
-                                for (int x = 0; x < 2; ++x) {
-                                    const uint32_t w = bits[x] >> (2 * cg);
-#pragma unroll
-                                    for (int k = 0; k < 4; ++k) {
-                                        if (!(w >> (8 * k) & 1u)) s[x][4 * k + 2 * e] = 0xff800000u;
-                                        if (!(w >> (8 * k + 1) & 1u)) s[x][4 * k + 2 * e + 1] = 0xff800000u;
-                                    }
+                                for (int e = 0; e < 2; ++e) {
+                                    const uint64_t sv = pair_of(__uint_as_float(s[4 * k + 2 * e]), __uint_as_float(s[4 * k + 2 * e + 1]));
+                                    const float2 p = of_pair(fma2(sv, pair_of(c2, c2), KEY ? cl : pair_of(nl[e], nl[e])));
+                                    s[4 * k + 2 * e] = __float_as_uint(ex2(p.x));
+                                    s[4 * k + 2 * e + 1] = __float_as_uint(ex2(p.y));
                                 }
                             }
                         }
-                        const uint64_t* const st = reinterpret_cast<const uint64_t*>(stats + (M % STAGES) * C::STAT_BYTES) + cg;
+                        wait(bT + 8, M & 1);
+                        __syncwarp();
+                        tc_fence_after();
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
                             uint32_t pp[8], pd[8];
+                            if (act) {
+                                uint32_t d[16];
+                                tmem_ld16x256_x4(tP + 32 * x, d);
+                                tc_wait_ld();
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                uint64_t cl, cd;
-                                if (KEY) {
-                                    cl = st[4 * (4 * x + k)];
-                                    cd = st[32 + 4 * (4 * x + k)];
-                                }
+                                for (int k = 0; k < 4; ++k) {
+                                    uint64_t cd;
+                                    if (KEY) cd = st[WIDTH / 2 + 4 * (4 * x + k)];
 #pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const uint64_t sv = pair_of(__uint_as_float(s[x][4 * k + 2 * e]), __uint_as_float(s[x][4 * k + 2 * e + 1]));
-                                    const uint64_t dv = pair_of(__uint_as_float(d[x][4 * k + 2 * e]), __uint_as_float(d[x][4 * k + 2 * e + 1]));
-                                    float2 p = of_pair(fma2(sv, pair_of(c2, c2), KEY ? cl : pair_of(nl[e], nl[e])));
-                                    p.x = ex2(p.x);
-                                    p.y = ex2(p.y);
-                                    if (KEY) pp[2 * k + e] = pack16<TYPE>(p.x, p.y);
-                                    const float2 g = of_pair(mul2(pair_of(p.x, p.y), fma2(dv, pair_of(1.f, 1.f), KEY ? cd : pair_of(nd[e], nd[e]))));
-                                    pd[2 * k + e] = pack16<TYPE>(g.x, g.y);
+                                    for (int e = 0; e < 2; ++e) {
+                                        const int i = 16 * x + 4 * k + 2 * e;
+                                        const uint64_t dv = pair_of(__uint_as_float(d[4 * k + 2 * e]), __uint_as_float(d[4 * k + 2 * e + 1]));
+                                        const uint64_t p = pair_of(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+                                        const float2 g = of_pair(mul2(p, fma2(dv, pair_of(1.f, 1.f), KEY ? cd : pair_of(nd[e], nd[e]))));
+                                        if (KEY) pp[2 * k + e] = pack16<TYPE>(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+                                        pd[2 * k + e] = pack16<TYPE>(g.x, g.y);
+                                    }
                                 }
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) pp[i] = pd[i] = 0u;
                             }
-                            // over what this warp has read: the first half's numbers lie in the first quarter of the buffer
-                            if (KEY) tmem_st16x128_x4(tS + 16 * x, pp);
-                            tmem_st16x128_x4(tP + 16 * x, pd);
+                            if (KEY) tmem_st16x128_x4(tP + 32 * x, pp);
+                            tmem_st16x128_x4(tP + 32 * x + 16, pd);
                         }
-                    } else {
-                        uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            if (KEY) tmem_st16x128_x4(tS + 16 * x, zero);
-                            tmem_st16x128_x4(tP + 16 * x, zero);
-                        }
+                        tc_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bP + 8);
                     }
-                    tc_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bP + 8 * buf);
+                } else {
+                    for (int j = 0; j < n; ++j, at.next(per_head)) {
+                        const uint32_t M = N + j;
+                        if ((int)(M & 1) != set) continue;
+                        int col0 = 0;
+                        bool act = true, compare = false;
+                        if ((uint32_t)(at.j - free_from) >= free_count) {
+                            col0 = 64 * u.blocks.at(at.j);
+                            const int4 whole = u.whole[group];
+                            const int3 reach = u.reach[group];
+                            act = (col0 < reach.y && col0 + 64 > reach.x) || col0 < reach.z;
+                            compare = !((col0 >= whole.x && col0 + 64 <= whole.y) || (col0 >= whole.z && col0 + 64 <= whole.w));
+                        }
+                        const uint32_t buf = M % NBUF, tS = lane_addr + C::S_COL + C::BUF_COLS * buf, tP = tS + 64;
+                        if (j % ABORT_EVERY < 2 && __any_sync(0xffffffffu, ctl->abort_flag)) return;
+                        if (KEY) wait(bF + 8 * (M % STAGES), (M / STAGES) & 1);    // nlse and ndelta of the block, read below
+                        wait(bT + 8 * buf, (M / NBUF) & 1);
+                        __syncwarp();
+                        tc_fence_after();
+                        if (act) {
+                            uint32_t s[2][16], d[2][16];
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                tmem_ld16x256_x4(tS + 32 * x, s[x]);
+                                tmem_ld16x256_x4(tP + 32 * x, d[x]);
+                            }
+                            tc_wait_ld();
+                            if (compare) {
+                                hide(col0, [&](int x, int i) -> uint32_t& { return s[x][i]; });
+                            }
+                            const uint64_t* const st = reinterpret_cast<const uint64_t*>(stats + (M % STAGES) * C::STAT_BYTES) + cg;
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                uint32_t pp[8], pd[8];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    uint64_t cl, cd;
+                                    if (KEY) {
+                                        cl = st[4 * (4 * x + k)];
+                                        cd = st[32 + 4 * (4 * x + k)];
+                                    }
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        const uint64_t sv = pair_of(__uint_as_float(s[x][4 * k + 2 * e]), __uint_as_float(s[x][4 * k + 2 * e + 1]));
+                                        const uint64_t dv = pair_of(__uint_as_float(d[x][4 * k + 2 * e]), __uint_as_float(d[x][4 * k + 2 * e + 1]));
+                                        float2 p = of_pair(fma2(sv, pair_of(c2, c2), KEY ? cl : pair_of(nl[e], nl[e])));
+                                        p.x = ex2(p.x);
+                                        p.y = ex2(p.y);
+                                        if (KEY) pp[2 * k + e] = pack16<TYPE>(p.x, p.y);
+                                        const float2 g = of_pair(mul2(pair_of(p.x, p.y), fma2(dv, pair_of(1.f, 1.f), KEY ? cd : pair_of(nd[e], nd[e]))));
+                                        pd[2 * k + e] = pack16<TYPE>(g.x, g.y);
+                                    }
+                                }
+                                // over what this warp has read: the first half's numbers lie in the first quarter of the buffer
+                                if (KEY) tmem_st16x128_x4(tS + 16 * x, pp);
+                                tmem_st16x128_x4(tP + 16 * x, pd);
+                            }
+                        } else {
+                            uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                if (KEY) tmem_st16x128_x4(tS + 16 * x, zero);
+                                tmem_st16x128_x4(tP + 16 * x, zero);
+                            }
+                        }
+                        tc_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bP + 8 * buf);
+                    }
                 }
             };
             const bool key = u.key;
@@ -723,7 +896,7 @@ cudaError_t static_init() {
     return cudaSuccess;
 }
 
-int padded_rows(const rapid3_window* w) { return (w->n_q + 63) / 64 * 64; }
+int padded_rows(const rapid3_window* w) { return (w->n_q + 127) / 128 * 128; }
 int64_t stat_floats(const rapid3_window* w) { return (int64_t)w->B * w->H * padded_rows(w); }
 
 // Tiles of first tokens, and how many units share one: so many that none takes longer than half of what an SM has to do in the mean, all
