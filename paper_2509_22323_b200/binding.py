@@ -9,6 +9,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+import types
 from typing import Optional, Sequence
 
 import torch
@@ -117,6 +118,12 @@ def load() -> ctypes.CDLL:
     lib.rapid3_window_workspace_bytes.restype = ctypes.c_int64
     lib.rapid3_window_status.argtypes = [ctypes.POINTER(ci)]
     lib.rapid3_rotary_freqs.argtypes = [ci, ctypes.c_double, ci, ctypes.c_double, ci, ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double), f32p]
+    # the same calls with addresses in the place of the Rows: the functions below lay the rows of a call out in one array
+    lib.by_address = types.SimpleNamespace()
+    for name in ("rapid3_rotary", "rapid3_norm_rotary", "rapid3_norm_rotary_backward", "rapid3_window_attn", "rapid3_window_attn_backward"):
+        fn = lib[name]                             # a function object of its own
+        fn.argtypes = [vp if t is rows else t for t in getattr(lib, name).argtypes]
+        setattr(lib.by_address, name, fn)
     _lib = lib
     return lib
 
@@ -362,13 +369,6 @@ def rapid3_cache_step(x: torch.Tensor, o: torch.Tensor, delta: torch.Tensor, act
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
-def _rows(t: Optional[torch.Tensor]):
-    if t is None:
-        return None
-    sb, sh, sn, _ = t.stride()
-    return Rows(t.data_ptr(), sb, sh, sn)
-
-
 # The checks of the calls below cost a third of a small call on the host (13 us when they were written for brevity): tensor by tensor, each
 # attribute read once, and what is wrong said only when something is.
 def _device(what: str, like: torch.Tensor) -> int:
@@ -378,9 +378,19 @@ def _device(what: str, like: torch.Tensor) -> int:
     return dev
 
 
-def _check_like(what: str, name: str, t: Optional[torch.Tensor], dtype: torch.dtype, dev: int, shape):
-    if t is None or t.dtype is not dtype or t.get_device() != dev or t.shape != shape or t.stride(3) != 1:
-        raise ValueError(f"{what}: {name} must be {tuple(shape)} of {dtype} on CUDA device {dev} with adjacent channels")
+def _tensors(what: str, dtype: torch.dtype, dev: int, items):
+    """One rapid3_rows (data, stride_b, stride_h, stride_n) after the other for (name, tensor, shape)s, checked; the array, and its address: number i
+    lies 32 i behind it."""
+    words = []
+    for name, t, shape in items:
+        if t is None or t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+            raise ValueError(f"{what}: {name} must be {tuple(shape)} of {dtype} on CUDA device {dev}")
+        sb, sh, sn, sd = t.stride()
+        if sd != 1:
+            raise ValueError(f"{what}: {name} must have adjacent channels")
+        words += (t.data_ptr(), sb, sh, sn)
+    rows = array.array("q", words)                 # (a ctypes array takes 0.6 us more)
+    return rows, rows.buffer_info()[0]
 
 
 def _check_vector(what: str, name: str, t: Optional[torch.Tensor], n: int, dev: int, dtype=torch.float32):
@@ -433,24 +443,23 @@ class Rotary:
 
 
 def _heads(what: str, q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, like_q, like_k):
-    """The shape of Q and K (k may be None), after checking them and what is like them: (name, tensor)s.  Also the device."""
+    """The shape of Q and K (k may be None), after checking them and what is like them, (name, tensor)s; the device; and _tensors() of q, like_q, k, like_k."""
     shape, dtype, dev = q.shape, q.dtype, _device(what, q)
     kind = _TYPES.get(dtype)
     if kind is None or len(shape) != 4:
         raise ValueError(f"{what}: q must be [B, H, N, D] of bf16, fp16 or fp32")
     B, H, N, D = shape
     rotary.check(what, dev, B, N)
-    _check_like(what, "q", q, dtype, dev, shape)
-    for name, t in like_q:
-        _check_like(what, name, t, dtype, dev, shape)
+    items = [("q", q, shape)] + [(name, t, shape) for name, t in like_q]
     Hk = 0
     if k is not None:
         k_shape = k.shape
-        Hk = k_shape[1] if len(k_shape) == 4 else 0
-        _check_like(what, "k", k, dtype, dev, (B, Hk, N, D))
-        for name, t in like_k:
-            _check_like(what, name, t, dtype, dev, k_shape)
-    return Heads(kind, B, N, D, H, Hk), dev
+        if len(k_shape) != 4 or k_shape[0] != B or k_shape[2] != N or k_shape[3] != D:
+            raise ValueError(f"{what}: k must be [B, H, N, D] and differ from q in H only")
+        Hk = k_shape[1]
+        items += [("k", k, k_shape)] + [(name, t, k_shape) for name, t in like_k]
+    rows, at = _tensors(what, dtype, dev, items)
+    return Heads(kind, B, N, D, H, Hk), dev, rows, at
 
 
 def rapid3_rotary(q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, q_out: Optional[torch.Tensor] = None,
@@ -459,9 +468,9 @@ def rapid3_rotary(q: torch.Tensor, k: Optional[torch.Tensor], rotary: Rotary, q_
     backward: q and k are gradients of the outputs, and those of the inputs come back."""
     q_out = torch.empty_like(q) if q_out is None else q_out
     k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
-    shape, _ = _heads("rapid3_rotary", q, k, rotary, (("q_out", q_out),), (("k_out", k_out),))
-    _check(load().rapid3_rotary(shape, _rows(q), _rows(k), rotary.turn, int(backward), _rows(q_out), None if k is None else _rows(k_out), _stream()),
-           "rapid3_rotary")
+    shape, _, rows, at = _heads("rapid3_rotary", q, k, rotary, (("q_out", q_out),), (("k_out", k_out),))
+    k_at, kout_at = (None, None) if k is None else (at + 64, at + 96)
+    _check(load().by_address.rapid3_rotary(shape, at, k_at, rotary.turn, int(backward), at + 32, kout_at, _stream()), "rapid3_rotary")
     return q_out, k_out
 
 
@@ -471,12 +480,13 @@ def rapid3_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_gain: torch
     what = "rapid3_norm_rotary"
     q_out = torch.empty_like(q) if q_out is None else q_out
     k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
-    shape, dev = _heads(what, q, k, rotary, (("q_out", q_out),), (("k_out", k_out),))
+    shape, dev, rows, at = _heads(what, q, k, rotary, (("q_out", q_out),), (("k_out", k_out),))
     _check_vector(what, "q_gain", q_gain, shape.D, dev)
+    k_at = kout_at = None
     if k is not None:
         _check_vector(what, "k_gain", k_gain, shape.D, dev)
-    _check(load().rapid3_norm_rotary(shape, _rows(q), _rows(k), _ptr(q_gain), _ptr(k_gain), float(eps), rotary.turn, _rows(q_out),
-                                     None if k is None else _rows(k_out), _stream()), what)
+        k_at, kout_at = at + 64, at + 96
+    _check(load().by_address.rapid3_norm_rotary(shape, at, k_at, q_gain.data_ptr(), _ptr(k_gain), float(eps), rotary.turn, at + 32, kout_at, _stream()), what)
     return q_out, k_out
 
 
@@ -491,38 +501,37 @@ def rapid3_norm_rotary_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Ten
     dk = torch.empty_like(k) if dk is None and k is not None else dk
     dq_gain = torch.empty_like(q_gain) if dq_gain is None else dq_gain
     dk_gain = torch.empty_like(k_gain) if dk_gain is None and k is not None and k_gain is not None else dk_gain
-    shape, dev = _heads(what, q, k, rotary, (("dq_out", dq_out), ("dq", dq)), (("dk_out", dk_out), ("dk", dk)))
+    shape, dev, rows, at = _heads(what, q, k, rotary, (("dq_out", dq_out), ("dq", dq)), (("dk_out", dk_out), ("dk", dk)))
     for name, t in (("q_gain", q_gain), ("dq_gain", dq_gain)) + ((("k_gain", k_gain), ("dk_gain", dk_gain)) if k is not None else ()):
         _check_vector(what, name, t, shape.D, dev)
     lib = load()
     size = lib.rapid3_norm_rotary_workspace_bytes(shape)
     workspace = torch.empty(max(16, size), dtype=torch.uint8, device=q.device)
-    _check(lib.rapid3_norm_rotary_backward(shape, _rows(dq_out), None if k is None else _rows(dk_out), _rows(q), _rows(k), _ptr(q_gain),
-                                           _ptr(k_gain), float(eps), rotary.turn, _rows(dq), None if k is None else _rows(dk), _ptr(dq_gain),
-                                           None if k is None else _ptr(dk_gain), _ptr(workspace), size, _stream()), what)
+    k_at, dk_out_at, dk_at = (None, None, None) if k is None else (at + 96, at + 128, at + 160)
+    _check(lib.by_address.rapid3_norm_rotary_backward(shape, at + 32, dk_out_at, at, k_at, _ptr(q_gain), _ptr(k_gain), float(eps), rotary.turn, at + 64, dk_at,
+                                           _ptr(dq_gain), None if k is None else _ptr(dk_gain), _ptr(workspace), size, _stream()), what)
     return dq, dk, dq_gain, dk_gain
 
 
 def _window(what: str, q: torch.Tensor, k: torch.Tensor, like_q, like_k, left: int, right: int, n_sink: int, n_full: int,
             q_len: Optional[torch.Tensor], kv_len: Optional[torch.Tensor], softmax_scale: Optional[float]):
-    """The shape and rule of a windowed attention, after checking Q, K, the lengths and what is like Q and K: (name, tensor)s.  Also the device."""
+    """The shape and rule of a windowed attention, after checking Q, K, the lengths and what is like Q and K, (name, tensor)s; the device; and
+    _tensors() of q, like_q, k, like_k."""
     shape, k_shape, dtype, dev = q.shape, k.shape, q.dtype, _device(what, q)
     if len(shape) != 4 or len(k_shape) != 4 or (dtype is not torch.bfloat16 and dtype is not torch.float16):
         raise ValueError(f"{what}: q [B, H, n_q, D] and k [B, H_kv, n_kv, D] must be bf16 or fp16")
     B, H, n_q, D = shape
-    _, Hk, n_kv, _ = k_shape
-    _check_like(what, "q", q, dtype, dev, shape)
-    _check_like(what, "k", k, dtype, dev, (B, Hk, n_kv, D))
-    for name, t in like_q:
-        _check_like(what, name, t, dtype, dev, shape)
-    for name, t in like_k:
-        _check_like(what, name, t, dtype, dev, k_shape)
+    Bk, Hk, n_kv, Dk = k_shape
+    if Bk != B or Dk != D:
+        raise ValueError(f"{what}: q and k must agree in B and D")
+    rows, at = _tensors(what, dtype, dev, [("q", q, shape)] + [(name, t, shape) for name, t in like_q] + [("k", k, k_shape)] +
+                         [(name, t, k_shape) for name, t in like_k])
     if q_len is not None:
         _check_vector(what, "q_len", q_len, B, dev, torch.int32)
     if kv_len is not None:
         _check_vector(what, "kv_len", kv_len, B, dev, torch.int32)
     return Window(_TYPES[dtype], B, H, Hk, D, n_q, n_kv, int(left), int(right), int(n_sink), int(n_full),
-                  float(softmax_scale if softmax_scale is not None else D ** -0.5), _ptr(q_len), _ptr(kv_len)), dev
+                  float(softmax_scale if softmax_scale is not None else D ** -0.5), _ptr(q_len), _ptr(kv_len)), dev, rows, at
 
 
 def _check_lse(what: str, lse: Optional[torch.Tensor], q: torch.Tensor, dev: int):
@@ -538,10 +547,10 @@ def rapid3_window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: O
     Returns out (allocated, rows from q_len on unset, unless given) and lse (filled if given)."""
     what = "rapid3_window_attn"
     out = torch.empty_like(q) if out is None else out
-    shape, dev = _window(what, q, k, (("out", out),), (("v", v),), left, right, n_sink, n_full, q_len, kv_len, softmax_scale)
+    shape, dev, rows, at = _window(what, q, k, (("out", out),), (("v", v),), left, right, n_sink, n_full, q_len, kv_len, softmax_scale)
     if lse is not None:
         _check_lse(what, lse, q, dev)
-    _check(load().rapid3_window_attn(shape, _rows(q), _rows(k), _rows(v), _rows(out), _ptr(lse), _stream()), what)
+    _check(load().by_address.rapid3_window_attn(shape, at, at + 64, at + 96, at + 32, _ptr(lse), _stream()), what)
     return out, lse
 
 
@@ -553,14 +562,14 @@ def rapid3_window_attn_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     Rows from q_len and keys from kv_len on are left as they were.  The same call gives the same bits."""
     what = "rapid3_window_attn_backward"
     dq, dk, dv = (torch.empty_like(x) if g is None else g for x, g in ((q, dq), (k, dk), (v, dv)))
-    shape, dev = _window(what, q, k, (("out", out), ("dout", dout), ("dq", dq)), (("v", v), ("dk", dk), ("dv", dv)), left, right, n_sink, n_full,
-                         q_len, kv_len, softmax_scale)
+    shape, dev, rows, at = _window(what, q, k, (("out", out), ("dout", dout), ("dq", dq)), (("v", v), ("dk", dk), ("dv", dv)), left, right, n_sink,
+                                    n_full, q_len, kv_len, softmax_scale)
     _check_lse(what, lse, q, dev)
     lib = load()
     size = lib.rapid3_window_workspace_bytes(shape)
     workspace = torch.empty(max(16, size), dtype=torch.uint8, device=q.device)
-    _check(lib.rapid3_window_attn_backward(shape, _rows(q), _rows(k), _rows(v), _rows(out), _ptr(lse), _rows(dout), _rows(dq), _rows(dk), _rows(dv),
-                                           _ptr(workspace), size, _stream()), what)
+    _check(lib.by_address.rapid3_window_attn_backward(shape, at, at + 128, at + 160, at + 32, _ptr(lse), at + 64, at + 96, at + 192, at + 224, _ptr(workspace),
+                                           size, _stream()), what)
     return dq, dk, dv
 
 
