@@ -340,7 +340,7 @@ int rapid3_rotary_freqs(int channels, double base, int scaling, double factor, i
  *     out = softmax(softmax_scale q k over the visible keys) v,   lse = log sum exp(softmax_scale q k) (natural, fp32)
  * A row that sees no key gets zeros and lse = -inf.  Scores, softmax and sums are fp32, the weights are rounded to the tensors' type
  * for the product with V.  Query head h reads key head h / (H / H_kv).
- * No context and, but for the backward pass's, no workspace; asynchronous on `stream`; nothing is allocated; one launch (backward: three).
+ * No context and, but for the backward pass's, no workspace; asynchronous on `stream`; nothing is allocated; one launch (backward: two to four).
  * Rows from q_len[b] on are neither read nor written, keys from kv_len[b] on do not count: what lies there may be anything.  Other
  * non-finite inputs give undefined results.
  */
@@ -361,7 +361,7 @@ int rapid3_window_attn(const rapid3_window* w, const rapid3_rows* q, const rapid
                        void* stream);
 
 /* Gradients dq, dk, dv from dout and what rapid3_window_attn read and wrote (lse is needed).  Outputs overlap nothing.  Keys that no
- * row sees get zeros; rows from q_len[b] on and keys from kv_len[b] on are left as they were.  B * H <= 65535.  workspace: device, 16-byte
+ * row sees get zeros; so do dq of a row that sees one key and its part of dk.  Rows from q_len[b] on and keys from kv_len[b] on are left as they were.  B * H <= 65535.  workspace: device, 16-byte
  * aligned, of at least the bytes that rapid3_window_workspace_bytes gives, used by one call at a time; nothing in it has to be set.  The
  * sums are taken in a fixed order: the same call gives the same bits. */
 int rapid3_window_attn_backward(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, const rapid3_rows* v, const rapid3_rows* out,

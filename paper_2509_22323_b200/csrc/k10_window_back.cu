@@ -14,6 +14,13 @@
 // products run beside the last one's results on their way out.  Tiles of first tokens see every row, far more than the others: where they
 // alone would keep a few SMs busy their blocks are shared out to several units, whose 32-bit results add_parts_kernel adds up.
 //
+// delta is made of the output that the caller has, which is rounded.  Of rows that see few keys, whose output is as large as a value, that
+// shows: dq and dk of causal sequences were 1.5 to 1.8 times as far off as the rounding of the weights alone makes them (2.7 times at five
+// tokens).  So tiles with rows that see fewer than EXACT_FROM keys have a launch of their own in front (`exact` row units), in which
+// e = the sum of a row's dS, as they are before their rounding, is found: what delta was short of.
+//     dQ = scale (sum dS K - e sum P K),   and delta + e is what the key units take
+// A row that sees one key has dS = 0: its delta is marked by infinity, and both kinds of unit write zeros for it.
+//
 // Roles (640 threads): warps 0-15 the element work: a warp owns 16 rows of the tile, a thread a quarter of two rows; warp 16 the producer
 // (TMA; rows behind a sequence's last, which are not the caller's to keep finite, are set to zero); warp 17 the UMMA issue; warp 18 the next unit.
 //
@@ -47,6 +54,7 @@ constexpr int ELEMENT_REGS = 104, LIGHT_REGS = 64;       // registers a thread o
 constexpr int TMEM_COLS = 512;
 constexpr int BLK_BYTES = 8192, XHALF_BYTES = 16384;
 constexpr int TAKE_AHEAD = 4, UNIT_USERS = WARPS + 2, ABORT_EVERY = 32;
+constexpr int EXACT_FROM = 256;                          // at 128 keys a row and more the error is below 1.5 times that of the weights alone
 constexpr int MAX_PARTS = 16, MAX_SLOTS = 2 * SM_COUNT;  // units of a shared-out tile; of all of them
 
 __device__ int status_word;
@@ -55,7 +63,7 @@ struct Params {
     Rule w;
     Rows dq, dk, dv;
     const float* nlse;           // [B][H][padded]: minus log sum exp in base 2; -inf: a row that has no P
-    const float* ndelta;         // minus delta
+    float* ndelta;               // minus delta; +inf: a row that sees one key (exact row units bring it up to date)
     float* partial;              // [slot][128][2 D]
     int padded;                  // query rows of a head in these, a multiple of 128
     int H, H_kv, group;
@@ -64,6 +72,8 @@ struct Params {
     int full_tiles;              // the first row tiles
     int sink_units, key_units, full_units;   // where the kinds end in the order of the units: sink tiles, other key tiles, full row tiles, other row tiles
     bool last_first;             // the last rows have the most keys
+    int few_tiles;               // the first row tiles, which may hold rows that see few keys
+    int pass;                    // 0: all units; 1: tiles with such rows; 2: all others
     float scale, scale_log2;
 };
 
@@ -101,10 +111,11 @@ struct Unit {
 struct __align__(16) Ctl {
     uint4 taken;
     unsigned long long taken_full, near_end, unit_full[2], unit_empty[2];
-    unsigned long long x_full, x_empty, tail_full, full[MAX_STAGES], empty[MAX_STAGES], t_full[3], p_full[3], done, drained, drain;
+    unsigned long long x_full, x_empty, tail_full, full[MAX_STAGES], empty[MAX_STAGES], t_full[3], p_full[3], done, drained, drain, pair[8];
     uint32_t tmem_base;
     volatile int abort_flag;
     Unit unit[2];
+    float short_of[WARPS][16];   // exact: of a warp's rows, its columns' part of e
 };
 template <int D>
 constexpr size_t smem_bytes() { return (size_t)Cfg<D>::DATA_BYTES + sizeof(Ctl) + 1024; }
@@ -145,6 +156,7 @@ __device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int grou
     whole = make_int4(0, 0, 0, 0);
     reach = make_int3(0, 0, 0);
     if (r0 > r1) return;
+    const bool one = u.keys == 1;                        // every block is looked at for rows that see one key, see `mark`
     if (u.key) {
         int lo, hi, from, to;
         rows_of_key(w, r0, u.rows, off, from, hi);       // from: the least; hi: the least unless the row is a first token
@@ -156,7 +168,7 @@ __device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int grou
         }
         int full_lo, full_hi;
         full_rows(w, u.rows, off, full_lo, full_hi);
-        whole = make_int4(lo, hi, full_lo, full_hi);
+        whole = one ? make_int4(0, 0, 0, 0) : make_int4(lo, hi, full_lo, full_hi);
         reach = make_int3(from, to, full_hi);
     } else {
         const int p0 = r0 + off, p1 = r1 + off;
@@ -170,7 +182,7 @@ __device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int grou
             w.seen(p1, u.keys, lo, x);
             if (p0 >= 0 && p1 < w.n_full) hi = u.keys;
         }
-        whole = make_int4(lo, hi, 0, min(w.n_sink, hi));
+        whole = one ? make_int4(0, 0, 0, 0) : make_int4(lo, hi, 0, min(w.n_sink, hi));
         reach = make_int3(from, to, min(w.n_sink, to));
     }
 }
@@ -192,11 +204,14 @@ __device__ __forceinline__ Blocks doubled(const Blocks& b) {
 
 __device__ __forceinline__ Unit unit_of(const Params& p, int B, int L, bool wide) {
     Unit u;
-    u.key = L < p.key_units;
+    u.key = p.pass != 1 && L < p.key_units;
     u.slot = -1;
     const int heads = B * (u.key ? p.H_kv : p.H);
     int part = 0, parts = 1, x, tile;
-    if (L < p.sink_units) {
+    if (p.pass == 1) {
+        x = L / p.few_tiles;
+        tile = L - x * p.few_tiles;
+    } else if (L < p.sink_units) {
         parts = p.parts;
         x = L / parts;
         part = L - x * parts;
@@ -219,6 +234,12 @@ __device__ __forceinline__ Unit unit_of(const Params& p, int B, int L, bool wide
     u.keys = p.w.keys(u.b);
     u.first = 128 * tile;
     u.end = u.key ? u.keys : u.rows;
+    if (!u.key && p.pass != 0) {
+        const int off = u.keys - u.rows;
+        // each tile in its pass (the rows of a tile that see the least are its first or its last)
+        if (u.first < u.end && (min(p.w.count(u.first + off, u.keys), p.w.count(min(u.first + 128, u.end) - 1 + off, u.keys)) < EXACT_FROM) != (p.pass == 1))
+            u.end = u.first;
+    }
     const int last = min(u.first + 128, u.end);
     u.blocks = u.first >= last ? Blocks{0, 0, 0} : u.key ? query_blocks(p.w, u.first, last, u.rows, u.keys)
                                                          : key_blocks(p.w, u.first, last, u.rows, u.keys);
@@ -245,7 +266,8 @@ struct Walk {
     }
 };
 
-template <int D, int TYPE>
+// EXACT: the build of pass 1, for exact row units alone.
+template <int D, int TYPE, bool EXACT>
 __global__ void __launch_bounds__(NTHREADS, 1)
 window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                    const __grid_constant__ CUtensorMap td, const __grid_constant__ Params prm, int B) {
@@ -263,6 +285,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
     const uint32_t bX = smem_u32(&ctl->x_full), bXE = smem_u32(&ctl->x_empty), bTail = smem_u32(&ctl->tail_full);
     const uint32_t bF = smem_u32(&ctl->full[0]), bE = smem_u32(&ctl->empty[0]), bT = smem_u32(&ctl->t_full[0]), bP = smem_u32(&ctl->p_full[0]);
     const uint32_t bD = smem_u32(&ctl->done), bDE = smem_u32(&ctl->drained);
+    const uint32_t bPair = smem_u32(&ctl->pair[0]);
     const uint32_t bUF = smem_u32(&ctl->unit_full[0]), bUE = smem_u32(&ctl->unit_empty[0]), bNE = smem_u32(&ctl->near_end), bTk = smem_u32(&ctl->taken_full);
 
     if (warp == 0) {
@@ -273,6 +296,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
             if (has(x, offsetof(Ctl, unit_empty), 2)) count = UNIT_USERS;
             if (has(x, offsetof(Ctl, p_full), 3)) count = WIDE ? WARPS : 8;     // one arrival per warp that works on the buffer
             if (has(x, offsetof(Ctl, drained), 1)) count = WARPS;
+            if (has(x, offsetof(Ctl, pair), 8)) count = 2;                      // both sets' warps of the rows
             mbar_init(smem_u32(ctl) + 8 * (at + x), count);
         }
         if (lane == 0) ctl->abort_flag = 0;
@@ -442,7 +466,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
             for (uint32_t i = 0; ok; ++i) {
                 if (!(ok = wait(bUF + 8 * (i & 1), (i >> 1) & 1))) break;
                 const int n = ctl->unit[i & 1].n;
-                const bool key = ctl->unit[i & 1].key;
+                const bool key = !EXACT && ctl->unit[i & 1].key;
                 if (n < 0) break;
                 if constexpr (WIDE) {
                     // w = 0: S from Y1, 1: dP from Y2
@@ -460,15 +484,15 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                         if (w == 1 && j == n - 1) tc_commit(bXE);
                         return true;
                     };
-                    // w = 0: += dS Y1, 1: dV += P Y2; every 32 columns of dP became 16 of P and 16 of dS
+                    // w = 0: += dS Y1, 1: dV += P Y2 (exact row unit: += P Y1); every 32 columns of dP became 16 of P and 16 of dS
                     auto second_product = [&](int j, int w) {
-                        const uint32_t s = (N + j) % STAGES, y = sY + s * C::STAGE_BYTES + w * C::Y_BYTES;
+                        const uint32_t s = (N + j) % STAGES, y = sY + s * C::STAGE_BYTES + (key && w ? C::Y_BYTES : 0);
                         tc_fence_after();
 #pragma unroll
                         for (int ks = 0; ks < 8; ++ks)
                             mma_ts(tmem_base + w * D, tmem_base + C::S_COL + 128 + (w ? 0 : 16) + (ks / 2) * 32 + (ks % 2) * 8,
                                    smem_desc_sw128(y + ks * 2048, C::YHALF_BYTES, 1024), idesc2, (j > 0 || ks > 0) ? 1u : 0u);
-                        tc_commit(bE + 8 * (w * STAGES + s));
+                        if (key || w == 0) tc_commit(bE + 8 * (w * STAGES + s));
                     };
                     if (n > 0) ok = wait(bX, n_x & 1) && first_product(0, 0) && first_product(0, 1);
                     for (int j = 0; ok && j < n; ++j) {
@@ -478,7 +502,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                         if (!(ok = wait(bP + 8, M & 1))) break;                // P and dS are there
                         // the first of a unit's second products overwrite the accumulators: those of the unit before have been read
                         if (j == 0 && n_x > 0 && !(ok = wait(bDE, (n_x - 1) & 1))) break;
-                        if (key) second_product(j, 1);
+                        if (key || EXACT) second_product(j, 1);
                         second_product(j, 0);
                         if (j + 1 < n && !(ok = first_product(j + 1, 1))) break;
                     }
@@ -510,14 +534,14 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                         if (j == 0 && n_x > 0 && !(ok = wait(bDE, (n_x - 1) & 1))) break;
                         tc_fence_after();
                         const uint32_t y = sY + s * C::STAGE_BYTES;
-                        // key unit: dK += dS^T Q, dV += P^T dO; row unit: dQ += dS K
+                        // key unit: dK += dS^T Q, dV += P^T dO; row unit: dQ += dS K, and (exact) P K
 #pragma unroll
                         for (int w = 0; w < 2; ++w)
-                            if (w == 0 || key)
+                            if (w == 0 || key || EXACT)
 #pragma unroll
                                 for (int ks = 0; ks < 4; ++ks)
                                     mma_ts(tmem_base + w * D, tmem_base + C::S_COL + C::BUF_COLS * (M % NBUF) + (w ? 0 : 64) + ks * 8,
-                                           smem_desc_sw128(y + w * C::Y_BYTES + ks * 2048, BLK_BYTES, 1024), idesc2, (j > 0 || ks > 0) ? 1u : 0u);
+                                           smem_desc_sw128(y + (key && w ? C::Y_BYTES : 0) + ks * 2048, BLK_BYTES, 1024), idesc2, (j > 0 || ks > 0) ? 1u : 0u);
                         tc_commit(bE + 8 * s);
                     }
                 }
@@ -536,13 +560,16 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
         const int set = warp >> 3, group = 2 * (warp & 3) + ((warp >> 2) & 1), cg = lane & 3;
         const uint32_t lane_addr = tmem_base + ((uint32_t)(16 * group) << 16);
         const float c2 = prm.scale_log2;
-        uint32_t N = 0, n_x = 0;
+        uint32_t N = 0, n_x = 0, n_pair = 0;
         for (uint32_t i = 0;; ++i) {
             if (!__all_sync(0xffffffffu, wait(bUF + 8 * (i & 1), (i >> 1) & 1))) break;
             const Unit& u = ctl->unit[i & 1];
             const int n = u.n;
             if (n < 0) break;
             // a unit's blocks, those of this warp's buffer
+            // (A build of its own for exact row units: with a third copy of this code in one the compiler kept the scores in local memory.)
+            const bool key = !EXACT && u.key;
+            float short_of[2] = {0.f, 0.f};              // exact: the sums of their dS
             auto element_work = [&](auto is_key) {
                 constexpr bool KEY = decltype(is_key)::value;
                 float nl[2] = {0.f, 0.f}, nd[2] = {0.f, 0.f};
@@ -588,6 +615,14 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                                 if (!(w >> (8 * k + 1) & 1u)) score(x, 4 * k + 2 * e + 1) = 0xff800000u;
                             }
                         }
+                    }
+                };
+                // dS of a column whose row sees one key is 0 (in a block that all keys of the warp see whole there is none)
+                auto mark = [&](auto looked_at, uint64_t cd, float2& g) {
+                    if (KEY && decltype(looked_at)::value) {
+                        const float2 d = of_pair(cd);
+                        if (d.x == INFINITY) g.x = 0.f;
+                        if (d.y == INFINITY) g.y = 0.f;
                     }
                 };
                 if constexpr (WIDE) {
@@ -636,13 +671,17 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                         wait(bT + 8, M & 1);
                         __syncwarp();
                         tc_fence_after();
+                        auto second_step = [&](auto looked_at) {
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            uint32_t pp[8], pd[8];
-                            if (act) {
-                                uint32_t d[16];
+                            for (int x = 0; x < 2; ++x) {
+                                uint32_t pp[8], pd[8], d[16];
                                 tmem_ld16x256_x4(tP + 32 * x, d);
                                 tc_wait_ld();
+                                if (EXACT) {             // (before dS, for registers)
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) pp[i] = pack16<TYPE>(__uint_as_float(s[16 * x + 2 * i]), __uint_as_float(s[16 * x + 2 * i + 1]));
+                                    tmem_st16x128_x4(tP + 32 * x, pp);
+                                }
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) {
                                     uint64_t cd;
@@ -652,17 +691,25 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                                         const int i = 16 * x + 4 * k + 2 * e;
                                         const uint64_t dv = pair_of(__uint_as_float(d[4 * k + 2 * e]), __uint_as_float(d[4 * k + 2 * e + 1]));
                                         const uint64_t p = pair_of(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-                                        const float2 g = of_pair(mul2(p, fma2(dv, pair_of(1.f, 1.f), KEY ? cd : pair_of(nd[e], nd[e]))));
+                                        float2 g = of_pair(mul2(p, fma2(dv, pair_of(1.f, 1.f), KEY ? cd : pair_of(nd[e], nd[e]))));
+                                        mark(looked_at, cd, g);
+                                        if (EXACT) short_of[e] += g.x + g.y;
                                         if (KEY) pp[2 * k + e] = pack16<TYPE>(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
                                         pd[2 * k + e] = pack16<TYPE>(g.x, g.y);
                                     }
                                 }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) pp[i] = pd[i] = 0u;
+                                if (KEY) tmem_st16x128_x4(tP + 32 * x, pp);
+                                tmem_st16x128_x4(tP + 32 * x + 16, pd);
                             }
-                            if (KEY) tmem_st16x128_x4(tP + 32 * x, pp);
-                            tmem_st16x128_x4(tP + 32 * x + 16, pd);
+                        };
+                        if (!act) {
+                            uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) tmem_st16x128_x4(tP + 16 * x, zero);
+                        } else if (KEY && compare) {
+                            second_step(std::true_type());
+                        } else {
+                            second_step(std::false_type());
                         }
                         tc_wait_st();
                         tc_fence_before();
@@ -700,37 +747,43 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                                 hide(col0, [&](int x, int i) -> uint32_t& { return s[x][i]; });
                             }
                             const uint64_t* const st = reinterpret_cast<const uint64_t*>(stats + (M % STAGES) * C::STAT_BYTES) + cg;
+                            auto both_steps = [&](auto looked_at) {
 #pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                uint32_t pp[8], pd[8];
+                                for (int x = 0; x < 2; ++x) {
+                                    uint32_t pp[8], pd[8];
 #pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    uint64_t cl, cd;
-                                    if (KEY) {
-                                        cl = st[4 * (4 * x + k)];
-                                        cd = st[32 + 4 * (4 * x + k)];
+                                    for (int k = 0; k < 4; ++k) {
+                                        uint64_t cl, cd;
+                                        if (KEY) {
+                                            cl = st[4 * (4 * x + k)];
+                                            cd = st[32 + 4 * (4 * x + k)];
+                                        }
+#pragma unroll
+                                        for (int e = 0; e < 2; ++e) {
+                                            const uint64_t sv = pair_of(__uint_as_float(s[x][4 * k + 2 * e]), __uint_as_float(s[x][4 * k + 2 * e + 1]));
+                                            const uint64_t dv = pair_of(__uint_as_float(d[x][4 * k + 2 * e]), __uint_as_float(d[x][4 * k + 2 * e + 1]));
+                                            float2 p = of_pair(fma2(sv, pair_of(c2, c2), KEY ? cl : pair_of(nl[e], nl[e])));
+                                            p.x = ex2(p.x);
+                                            p.y = ex2(p.y);
+                                            if (KEY || EXACT) pp[2 * k + e] = pack16<TYPE>(p.x, p.y);
+                                            float2 g = of_pair(mul2(pair_of(p.x, p.y), fma2(dv, pair_of(1.f, 1.f), KEY ? cd : pair_of(nd[e], nd[e]))));
+                                            mark(looked_at, cd, g);
+                                            if (EXACT) short_of[e] += g.x + g.y;
+                                            pd[2 * k + e] = pack16<TYPE>(g.x, g.y);
+                                        }
                                     }
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e) {
-                                        const uint64_t sv = pair_of(__uint_as_float(s[x][4 * k + 2 * e]), __uint_as_float(s[x][4 * k + 2 * e + 1]));
-                                        const uint64_t dv = pair_of(__uint_as_float(d[x][4 * k + 2 * e]), __uint_as_float(d[x][4 * k + 2 * e + 1]));
-                                        float2 p = of_pair(fma2(sv, pair_of(c2, c2), KEY ? cl : pair_of(nl[e], nl[e])));
-                                        p.x = ex2(p.x);
-                                        p.y = ex2(p.y);
-                                        if (KEY) pp[2 * k + e] = pack16<TYPE>(p.x, p.y);
-                                        const float2 g = of_pair(mul2(pair_of(p.x, p.y), fma2(dv, pair_of(1.f, 1.f), KEY ? cd : pair_of(nd[e], nd[e]))));
-                                        pd[2 * k + e] = pack16<TYPE>(g.x, g.y);
-                                    }
+                                    // over what this warp has read: the first half's numbers lie in the first quarter of the buffer
+                                    if (KEY || EXACT) tmem_st16x128_x4(tS + 16 * x, pp);
+                                    tmem_st16x128_x4(tP + 16 * x, pd);
                                 }
-                                // over what this warp has read: the first half's numbers lie in the first quarter of the buffer
-                                if (KEY) tmem_st16x128_x4(tS + 16 * x, pp);
-                                tmem_st16x128_x4(tP + 16 * x, pd);
-                            }
+                            };
+                            if (KEY && compare) both_steps(std::true_type());
+                            else both_steps(std::false_type());
                         } else {
                             uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
-                                if (KEY) tmem_st16x128_x4(tS + 16 * x, zero);
+                                if (KEY || EXACT) tmem_st16x128_x4(tS + 16 * x, zero);
                                 tmem_st16x128_x4(tP + 16 * x, zero);
                             }
                         }
@@ -741,9 +794,43 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                     }
                 }
             };
-            const bool key = u.key;
-            if (key) element_work(std::true_type());
-            else element_work(std::false_type());
+            if constexpr (EXACT) {
+                element_work(std::false_type());
+            } else {
+                if (key) element_work(std::true_type());
+                else element_work(std::false_type());
+            }
+            float nd[2] = {0.f, 0.f};                    // of a row unit, minus delta of the thread's two rows, again
+            if (!key) {
+                const int row = u.first + 16 * group + (lane >> 2);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (row + 8 * e < u.end) nd[e] = __ldcg(prm.ndelta + ((long long)u.b * prm.H + u.h) * prm.padded + row + 8 * e);
+            }
+            // e of the thread's two rows: of its lane quad's columns, then of both sets
+            float e_row[2] = {0.f, 0.f};
+            if constexpr (EXACT) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = short_of[e];
+                    x += __shfl_xor_sync(0xffffffffu, x, 1);
+                    x += __shfl_xor_sync(0xffffffffu, x, 2);
+                    if (cg == 0) ctl->short_of[warp][(lane >> 2) + 8 * e] = x;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bPair + 8 * group);
+                wait(bPair + 8 * group, n_pair++ & 1);
+                __syncwarp();
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = (lane >> 2) + 8 * e, low = warp & 7;
+                    e_row[e] = ctl->short_of[low][r] + ctl->short_of[low + 8][r];
+                    const int row = u.first + 16 * group + r;
+                    // (of a row that sees one key e is not a number, and its mark stays)
+                    if (set == 0 && cg == 0 && row < u.end && nd[e] != INFINITY)
+                        __stcg(prm.ndelta + ((long long)u.b * prm.H + u.h) * prm.padded + row, nd[e] - e_row[e]);
+                }
+            }
             // the results: of a key unit half of the warps dK, half dV; of a row unit half of dQ's channels each
             if (n > 0) wait(bD, n_x & 1);
             if (!__all_sync(0xffffffffu, !ctl->abort_flag)) break;
@@ -773,6 +860,20 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                                make_float2(__uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3])));
                     }
                     continue;
+                }
+                if constexpr (EXACT) {
+                    uint32_t pk[16];
+                    if (n > 0) {
+                        tmem_ld16x256_x4(lane_addr + D + ch * 32, pk);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(fmaf(-e_row[e >> 1 & 1], __uint_as_float(pk[e]), __uint_as_float(o[e])));
+                    }
+                }
+                if (!key) {                              // rows that see one key
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (nd[e >> 1 & 1] == INFINITY) o[e] = 0u;
                 }
                 uint32_t w_lo[4], w_hi[4];
 #pragma unroll
@@ -844,7 +945,7 @@ __global__ void __launch_bounds__(256) row_stats_kernel(const Rule w, const Rows
     constexpr int AT_ONCE = 4, PER = 256 / LPR;          // rows of a lane, rows of a pass
     const int lane = threadIdx.x % LPR, i0 = blockIdx.x * (PER * AT_ONCE) + threadIdx.x / LPR, h = blockIdx.y % H, b = blockIdx.y / H;
     grid_dependency_wait();
-    const int rows = w.rows(b);
+    const int rows = w.rows(b), keys = w.keys(b);
     uint4 o[AT_ONCE], d[AT_ONCE];
     float l[AT_ONCE];
 #pragma unroll
@@ -874,7 +975,7 @@ __global__ void __launch_bounds__(256) row_stats_kernel(const Rule w, const Rows
         if (lane == 0 && i < padded) {
             const long long at = ((long long)b * H + h) * padded + i;
             nlse[at] = l[x] == -INFINITY ? -INFINITY : l[x] * -1.4426950408889634f;
-            ndelta[at] = -sum;
+            ndelta[at] = i < rows && w.count(i + keys - rows, keys) == 1 ? INFINITY : -sum;
         }
     }
 }
@@ -887,11 +988,13 @@ cudaError_t static_init() {
     if (e != cudaSuccess) return e;
     const uint64_t bit = 1ull << (dev & 63);
     if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
-    if ((e = cudaFuncSetAttribute(window_back_kernel<D, TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>())) != cudaSuccess) return e;
-    // the warps that take registers wait for them: a build that is launched with fewer would wait for good
-    cudaFuncAttributes attr;
-    if ((e = cudaFuncGetAttributes(&attr, window_back_kernel<D, TYPE>)) != cudaSuccess) return e;
-    if (attr.numRegs * NTHREADS < 32 * (WARPS * ELEMENT_REGS + 4 * LIGHT_REGS)) return cudaErrorInvalidKernelImage;
+    for (const void* kernel : {(const void*)window_back_kernel<D, TYPE, false>, (const void*)window_back_kernel<D, TYPE, true>}) {
+        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>())) != cudaSuccess) return e;
+        // the warps that take registers wait for them: a build that is launched with fewer would wait for good
+        cudaFuncAttributes attr;
+        if ((e = cudaFuncGetAttributes(&attr, kernel)) != cudaSuccess) return e;
+        if (attr.numRegs * NTHREADS < 32 * (WARPS * ELEMENT_REGS + 4 * LIGHT_REGS)) return cudaErrorInvalidKernelImage;
+    }
     done.fetch_or(bit, std::memory_order_release);
     return cudaSuccess;
 }
@@ -913,6 +1016,25 @@ void sharing(const rapid3_window* w, int& sink_tiles, int& parts) {
                             (long long)w->B * w->H * row_tiles * std::min(key_blocks, near / 64 + (w->n_sink + 63) / 64);
     const long long most = std::max<long long>(48, total / SM_COUNT / 2), slots = (long long)sink_tiles * w->B * w->H_kv;
     parts = (int)std::min<long long>(std::min<long long>(MAX_PARTS, (sink + most - 1) / most), std::max<long long>(1, MAX_SLOTS / slots));
+}
+
+// The first row tiles of which rows may see fewer than EXACT_FROM keys: none, some at the beginning, or (where that is not for the host to say)
+// all.  every: each tile surely holds such rows.
+int few_tiles(const rapid3_window* w, bool& every) {
+    const int tiles = (w->n_q + 127) / 128;
+    every = false;
+    if (w->q_len || w->kv_len || w->n_q > w->n_kv) return tiles;
+    Rule rule = rule_of(w);
+    auto few = [&](int tile) {
+        const int off = w->n_kv - w->n_q, first = 128 * tile + off, last = std::min(128 * tile + 127, w->n_q - 1) + off;
+        return std::min(rule.count(first, w->n_kv), rule.count(last, w->n_kv)) < EXACT_FROM;
+    };
+    int n = 0;
+    if (w->left >= 0 && w->right >= 0 && (long long)w->left + w->right + 1 + w->n_sink < EXACT_FROM && w->n_full == 0) n = tiles;
+    while (n < tiles && few(n)) ++n;
+    every = n == tiles;
+    // the rows behind see a whole window, but for those at the end
+    return n < tiles && few(tiles - 1) ? tiles : n;
 }
 
 template <int D, int TYPE>
@@ -957,7 +1079,15 @@ int run(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, cons
     if (launch_kernel(row_stats_kernel<D, TYPE>, dim3((p.padded + PER - 1) / PER, heads), dim3(256), 0, s, p.w, rows_arg(out), rows_arg(dout), lse,
                       stats, ndelta, w->H, p.padded) != cudaSuccess)
         return RAPID3_ERR_CUDA;
-    if (launch_kernel(window_back_kernel<D, TYPE>, dim3(units), dim3(NTHREADS), smem_bytes<D>(), s, tq, tk, tv, td, p, w->B) != cudaSuccess)
+    bool every;
+    p.few_tiles = few_tiles(w, every);
+    p.pass = p.few_tiles > 0 ? 1 : 0;
+    if (p.pass == 1) {
+        if (launch_kernel(window_back_kernel<D, TYPE, true>, dim3(heads * p.few_tiles), dim3(NTHREADS), smem_bytes<D>(), s, tq, tk, tv, td, p, w->B) != cudaSuccess)
+            return RAPID3_ERR_CUDA;
+        p.pass = 2;
+    }
+    if (launch_kernel(window_back_kernel<D, TYPE, false>, dim3(every ? p.key_units : units), dim3(NTHREADS), smem_bytes<D>(), s, tq, tk, tv, td, p, w->B) != cudaSuccess)
         return RAPID3_ERR_CUDA;
     const int shared = key_heads * p.sink_tiles;
     if (p.parts > 1 && launch_kernel(add_parts_kernel<D, TYPE>, dim3((shared * 128 * (2 * D / 8) + 255) / 256), dim3(256), 0, s, p, w->B, shared) != cudaSuccess)

@@ -727,7 +727,7 @@ int check(const rapid3_window* w) {
         (long long)w->B * w->H_kv * ((w->n_kv + 127ll) / 128) > (1 << 30))
         return RAPID3_ERR_UNSUPPORTED;
     if (w->left < -1 || w->right < -1 || w->n_sink < 0 || w->n_full < 0) return RAPID3_ERR_INVALID_ARG;
-    if (!(w->softmax_scale > 0.f) || !isfinite(w->softmax_scale)) return RAPID3_ERR_INVALID_ARG;
+    if (!(w->softmax_scale > 0.f) || !isfinite(w->softmax_scale * 1.4426950408889634f)) return RAPID3_ERR_INVALID_ARG;
     return RAPID3_OK;
 }
 

@@ -27,16 +27,21 @@ struct Rule {
     __device__ __forceinline__ int rows(int b) const { return q_len ? min(max(__ldcg(q_len + b), 0), n_q) : n_q; }
     __device__ __forceinline__ int keys(int b) const { return kv_len ? min(max(__ldcg(kv_len + b), 0), n_kv) : n_kv; }
     // The row at position p sees the keys j < hi with j >= lo or j < n_sink.  near: as if no row were full.
-    __device__ __forceinline__ void near(int p, int keys, int& lo, int& hi) const {
+    __host__ __device__ __forceinline__ void near(int p, int keys, int& lo, int& hi) const {
         lo = left < 0 ? 0 : max(p - left, 0);
         hi = right < 0 ? keys : min(keys, max(p + right + 1, 0));
     }
-    __device__ __forceinline__ void seen(int p, int keys, int& lo, int& hi) const {
+    __host__ __device__ __forceinline__ void seen(int p, int keys, int& lo, int& hi) const {
         near(p, keys, lo, hi);
         if ((unsigned)p < (unsigned)n_full) {
             lo = 0;
             hi = keys;
         }
+    }
+    __host__ __device__ __forceinline__ int count(int p, int keys) const {
+        int lo, hi;
+        seen(p, keys, lo, hi);
+        return max(hi - lo, 0) + max(min(n_sink, min(lo, hi)), 0);
     }
     // The same of the 64 keys from key0 on, as bits.
     __device__ __forceinline__ void seen_bits(int p, int keys, int key0, uint32_t (&bits)[2]) const {

@@ -23,7 +23,7 @@ def call(fn="rapid3_window_attn", shape=None, rows=None, q=True, lse=4096, works
 
 BAD = [(-2, dict(type=2)), (-1, dict(type=3)), (-2, dict(D=96)), (-1, dict(B=0)), (-1, dict(H=0)), (-1, dict(H_kv=0)), (-1, dict(H=5)), (-1, dict(n_q=0)),
        (-1, dict(n_kv=0)), (-2, dict(n_q=1 << 30)), (-2, dict(n_kv=1 << 30)), (-2, dict(H=131072)), (-1, dict(left=-2)), (-1, dict(right=-2)),
-       (-1, dict(n_sink=-1)), (-1, dict(n_full=-1)), (-1, dict(softmax_scale=0.0)), (-1, dict(softmax_scale=math.nan)), (-2, dict(B=1 << 20, n_kv=1 << 22))]
+       (-1, dict(n_sink=-1)), (-1, dict(n_full=-1)), (-1, dict(softmax_scale=0.0)), (-1, dict(softmax_scale=math.nan)), (-1, dict(softmax_scale=3e38)), (-2, dict(B=1 << 20, n_kv=1 << 22))]
 
 
 @pytest.mark.parametrize("fn", ["rapid3_window_attn", "rapid3_window_attn_backward"])
