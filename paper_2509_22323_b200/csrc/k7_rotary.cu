@@ -394,25 +394,25 @@ __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constan
     }
 }
 
-// The gains' gradients: the thread blocks' sums, added up in fp64 in a fixed order.  32 channels a thread block.
-__global__ void __launch_bounds__(1024) gain_kernel(const float* partial, int blocks, int D, float* dq_gain, float* dk_gain) {
-    __shared__ double sums[32][33];
+// The gains' gradients: the thread blocks' sums, added up in fp64 in a fixed order.  Eight channels a thread block.
+__global__ void __launch_bounds__(512) gain_kernel(const float* partial, int blocks, int D, float* dq_gain, float* dk_gain) {
+    __shared__ double sums[16][8];
     grid_dependency_wait();
     grid_dependency_launch();
-    const int x = threadIdx.x % 32, y = threadIdx.x / 32, channel = blockIdx.x * 32 + x;
+    const int x = threadIdx.x % 8, y = threadIdx.x / 8, channel = blockIdx.x * 8 + x;    // 2 D is a multiple of 32
     double s = 0.0;
-    if (channel < 2 * D)
-        for (int b = y; b < blocks; b += 32) s += (double)__ldcg(partial + (size_t)b * 2 * D + channel);
-    sums[y][x] = s;
+#pragma unroll 8
+    for (int b = y; b < blocks; b += 64) s += (double)__ldcg(partial + (size_t)b * 2 * D + channel);
+    s += __shfl_xor_sync(0xffffffffu, s, 8);
+    s += __shfl_xor_sync(0xffffffffu, s, 16);
+    if (threadIdx.x % 32 < 8) sums[threadIdx.x / 32][x] = s;
     __syncthreads();
-    s = sums[x][y];
+    if (threadIdx.x >= 8) return;
+    s = 0.0;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    const int mine = blockIdx.x * 32 + y;
-    if (x == 0 && mine < 2 * D) {
-        float* to = mine < D ? dq_gain + mine : dk_gain ? dk_gain + mine - D : nullptr;
-        if (to) *to = (float)s;
-    }
+    for (int w = 0; w < 16; ++w) s += sums[w][x];
+    float* to = channel < D ? dq_gain + channel : dk_gain ? dk_gain + channel - D : nullptr;
+    if (to) *to = (float)s;
 }
 
 template <int TYPE, int LPR, bool HALVES>
@@ -531,7 +531,7 @@ int run_rotary(const rapid3_heads* s, const rapid3_rows* const (&in)[2], const r
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (launch_kernel(kernel, dim3(blocks, groups), dim3(32 * WARPS), ring_bytes(s->type, grads), st, a) != cudaSuccess)
         return RAPID3_ERR_CUDA;
-    if (grads && launch_kernel(gain_kernel, dim3((2 * s->D + 31) / 32), dim3(1024), 0, st, (const float*)a.partial, blocks * groups, s->D, dq_gain,
+    if (grads && launch_kernel(gain_kernel, dim3(2 * s->D / 8), dim3(512), 0, st, (const float*)a.partial, blocks * groups, s->D, dq_gain,
                                dk_gain) != cudaSuccess)
         return RAPID3_ERR_CUDA;
     return RAPID3_OK;
