@@ -32,8 +32,9 @@
 // (0: dK or dQ, 128: dV, 256: S, 384: dP), and the element work goes in two steps: P from S, which stays in registers, so that the next
 // block's S can follow at once; then dS from dP, and both, rounded, over the dP that the warp has read.  What is left in one chain is dS, the
 // second products and the next block's dP (2000 cycles of a block's 3300); the element work takes as long, 350 instructions a warp at one in
-// nine cycles.  Training pass of 4095 causal tokens, 32 heads on 8, window of 1024: blocks of 64 355 us, of 128 with P over S 349, so 335.  The exponential
-// unit is not what it waits for: with a quarter or half of the powers on the fma units it took 340 to 343 us.
+// nine cycles.  Training pass of 4095 causal tokens, 32 heads on 8, window of 1024: blocks of 64 355 us, of 128 with P over S 349, so 335, and 356 with the
+// launch for rows of few keys; 398 in a hot card's long run (one at a time: forward 89, row_stats_kernel 16, that launch 15, this one 267).  211 GFLOP of seen pairs.
+// The exponential unit is not what it waits for: with a quarter or half of the powers on the fma units the 335 were 340 to 343.
 // Every mbarrier wait is bounded, as in K8.
 #include <math.h>
 #include <stddef.h>
