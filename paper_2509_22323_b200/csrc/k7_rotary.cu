@@ -16,7 +16,7 @@
 //
 // Measured at D = 128, bf16: Q and K of three sequences of 4608 tokens and 24 heads, normed and turned, 339.7 MB in 70 us, 4.9 TB/s, 0.74 of a
 // copy's rate; gradients of 32 + 8 heads of 8191 tokens, gains' included, 251.6 MB in 56 us, 4.5 TB/s.  At D = 64, fp16: gradients of 24 + 24 heads
-// of two sequences of 4429 tokens, 163 MB in 41 us.  The instructions are issued in 45 of 100 cycles.  Sixteen channels a lane instead of eight take
+// of two sequences of 4429 tokens, 163 MB in 40 us.  The instructions are issued in 45 of 100 cycles.  Sixteen channels a lane instead of eight take
 // half of the shuffles and 115 to 155 registers: 71 us, and 53 for the 41 of the gradients.  Single tokens: 9 to 10 us a call, the launch.
 #include <math.h>
 
@@ -182,6 +182,9 @@ __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constan
     char* const ring_at = ring + warp * (DEPTH * STREAMS * STEP) + (lane / LPR) * ROW;
     const uint32_t my_ring = ptx::smem_u32(ring_at);
     grid_dependency_wait();
+    // gain_kernel's few thread blocks may be there and wait where an SM has room (gradients of 24 + 24 heads at D = 64: 43.6 -> 41.6 us); other
+    // launches that wait beside this one only take its SMs' room (rotation alone 12.7 -> 13.6)
+    if (GRADS) grid_dependency_launch();
     for (int tile = blockIdx.x; tile < p.n_tiles; tile += gridDim.x) {
         const int b = tile / p.tiles, n = ((tile - b * p.tiles) << p.log_tokens) + mine;
         const bool live = n < p.N && here;
@@ -371,7 +374,7 @@ __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constan
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
     }
-    grid_dependency_launch();
+    if (!GRADS) grid_dependency_launch();
     if constexpr (GRADS) {
         // the lanes' sums of the thread block, in a fixed order: rows of a warp, then warps; through the ring's memory
         static_assert(sizeof(float) * WARPS * 2 * MAX_D <= ring_bytes(TYPE, true), "the sums fit the ring");
