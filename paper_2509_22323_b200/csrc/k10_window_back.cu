@@ -157,8 +157,8 @@ __device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int grou
     whole = make_int4(0, 0, 0, 0);
     reach = make_int3(0, 0, 0);
     if (r0 > r1) return;
-    const bool one = u.keys == 1;                        // every block is looked at for rows that see one key, see `mark`
     if (u.key) {
+        const bool lone = r0 == r1;                      // every block is looked at for rows that see this key alone, see `mark`
         int lo, hi, from, to;
         rows_of_key(w, r0, u.rows, off, from, hi);       // from: the least; hi: the least unless the row is a first token
         rows_of_key(w, r1, u.rows, off, lo, to);
@@ -169,7 +169,7 @@ __device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int grou
         }
         int full_lo, full_hi;
         full_rows(w, u.rows, off, full_lo, full_hi);
-        whole = one ? make_int4(0, 0, 0, 0) : make_int4(lo, hi, full_lo, full_hi);
+        whole = lone ? make_int4(0, 0, 0, 0) : make_int4(lo, hi, full_lo, full_hi);
         reach = make_int3(from, to, full_hi);
     } else {
         const int p0 = r0 + off, p1 = r1 + off;
@@ -183,7 +183,7 @@ __device__ __forceinline__ void bounds_of(const Rule& w, const Unit& u, int grou
             w.seen(p1, u.keys, lo, x);
             if (p0 >= 0 && p1 < w.n_full) hi = u.keys;
         }
-        whole = one ? make_int4(0, 0, 0, 0) : make_int4(lo, hi, 0, min(w.n_sink, hi));
+        whole = make_int4(lo, hi, 0, min(w.n_sink, hi));
         reach = make_int3(from, to, min(w.n_sink, to));
     }
 }
@@ -618,7 +618,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                         }
                     }
                 };
-                // dS of a column whose row sees one key is 0 (in a block that all keys of the warp see whole there is none)
+                // dS of a column whose row sees one key is 0 (where every row of a block sees all of the warp's keys, two at least, there is none)
                 auto mark = [&](auto looked_at, uint64_t cd, float2& g) {
                     if (KEY && decltype(looked_at)::value) {
                         const float2 d = of_pair(cd);
