@@ -353,7 +353,8 @@ __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constan
                         ss += __shfl_xor_sync(0xffffffffu, ss, o);
                         dot += __shfl_xor_sync(0xffffffffu, dot, o);
                     }
-                    const float r1 = rsqrtf(ss * p.inv_D + p.eps);
+                    // (a slot without a row counts for nothing, also where eps is 0 and 1 / sqrt(0) infinite)
+                    const float r1 = left > 0 ? rsqrtf(ss * p.inv_D + p.eps) : 0.f;
                     const uint64_t r = twice(r1), m = twice(-dot * r1 * r1 * p.inv_D);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
