@@ -116,7 +116,9 @@ struct __align__(16) Ctl {
     uint32_t tmem_base;
     volatile int abort_flag;
     Unit unit[2];
-    float short_of[WARPS][16];   // exact: of a warp's rows, its columns' part of e
+    // exact: of a warp's rows, its columns' part of e.  By turns: a warp may be a unit ahead of the one it shares rows with, not two, since a Unit is
+    // written again only when all have left the one before in its place.
+    float short_of[2][WARPS][16];
 };
 template <int D>
 constexpr size_t smem_bytes() { return (size_t)Cfg<D>::DATA_BYTES + sizeof(Ctl) + 1024; }
@@ -816,7 +818,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
                     float x = short_of[e];
                     x += __shfl_xor_sync(0xffffffffu, x, 1);
                     x += __shfl_xor_sync(0xffffffffu, x, 2);
-                    if (cg == 0) ctl->short_of[warp][(lane >> 2) + 8 * e] = x;
+                    if (cg == 0) ctl->short_of[i & 1][warp][(lane >> 2) + 8 * e] = x;
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bPair + 8 * group);
@@ -825,7 +827,7 @@ window_back_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = (lane >> 2) + 8 * e, low = warp & 7;
-                    e_row[e] = ctl->short_of[low][r] + ctl->short_of[low + 8][r];
+                    e_row[e] = ctl->short_of[i & 1][low][r] + ctl->short_of[i & 1][low + 8][r];
                     const int row = u.first + 16 * group + r;
                     // (of a row that sees one key e is not a number, and its mark stays)
                     if (set == 0 && cg == 0 && row < u.end && nd[e] != INFINITY)
