@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constan
     // gain_kernel's few thread blocks may be there and wait where an SM has room (gradients of 24 + 24 heads at D = 64: 43.6 -> 41.6 us); other
     // launches that wait beside this one only take its SMs' room (rotation alone 12.7 -> 13.6)
     if (GRADS) grid_dependency_launch();
-    for (int tile = blockIdx.x; tile < p.n_tiles; tile += gridDim.x) {
-        const int b = tile / p.tiles, n = ((tile - b * p.tiles) << p.log_tokens) + mine;
+    for (uint32_t tile = blockIdx.x; tile < (uint32_t)p.n_tiles; tile += gridDim.x) {      // (a tile and a grid may be 2^31 - 1, their sum is no int)
+        const int b = (int)tile / p.tiles, n = (((int)tile - b * p.tiles) << p.log_tokens) + mine;
         const bool live = n < p.N && here;
         // this thread block's heads among those of Q and then K; a slot's steps through them
         int first_head[2], heads[2], steps[2];
