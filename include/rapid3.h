@@ -370,7 +370,8 @@ int rapid3_window_attn_backward(const rapid3_window* w, const rapid3_rows* q, co
 int64_t rapid3_window_workspace_bytes(const rapid3_window* w);
 
 /* The current device's status word of the two calls above (RAPID3_OK, or RAPID3_ERR_TIMEOUT after a bounded wait inside a kernel ran
- * out, whose results are then incomplete); clears it.  Synchronises the device. */
+ * out, whose results are then incomplete); clears it.  Synchronises the device, all of its streams.  The word is one for all calls of a device,
+ * of every stream and host thread: it does not say whose results are incomplete, and whoever asks first clears it. */
 int rapid3_window_status(int* status);
 
 /* Device pointers of the workspace rapid3_gated_step fills (any may be NULL): layouts as in

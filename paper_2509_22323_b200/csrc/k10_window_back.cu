@@ -1100,10 +1100,9 @@ int run(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, cons
 
 }  // namespace
 
-cudaError_t window_back_status(int* value) {
-    cudaError_t e = cudaMemcpyFromSymbol(value, status_word, sizeof(int));
+cudaError_t window_back_status(int* value, bool clear) {
     const int zero = 0;
-    return e != cudaSuccess ? e : cudaMemcpyToSymbol(status_word, &zero, sizeof(int));
+    return clear ? cudaMemcpyToSymbol(status_word, &zero, sizeof(int)) : cudaMemcpyFromSymbol(value, status_word, sizeof(int));
 }
 
 extern "C" {

@@ -768,16 +768,18 @@ int tensor_map(const rapid3_window* w, const rapid3_rows* t, int heads, int n, C
 
 }  // namespace window
 
-cudaError_t window_back_status(int* value);              // k10_window_back.cu
+cudaError_t window_back_status(int* value, bool clear);  // k10_window_back.cu
 
 extern "C" {
 
 int rapid3_window_status(int* status) {
     if (!status) return RAPID3_ERR_INVALID_ARG;
+    // Copies from and to symbols wait for the streams that the legacy default stream waits for, and no others.
     int forward = 0, back = 0;
     const int zero = 0;
-    if (cudaMemcpyFromSymbol(&forward, status_word, sizeof(int)) != cudaSuccess || cudaMemcpyToSymbol(status_word, &zero, sizeof(int)) != cudaSuccess ||
-        window_back_status(&back) != cudaSuccess) {
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&forward, status_word, sizeof(int)) != cudaSuccess ||
+        window_back_status(&back, false) != cudaSuccess || (forward && cudaMemcpyToSymbol(status_word, &zero, sizeof(int)) != cudaSuccess) ||
+        (back && window_back_status(&back, true) != cudaSuccess)) {
         cudaGetLastError();
         return RAPID3_ERR_CUDA;
     }
