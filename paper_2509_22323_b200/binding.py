@@ -499,7 +499,7 @@ def rapid3_norm_rotary_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Ten
     what = "rapid3_norm_rotary_backward"
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None and k is not None else dk
-    dq_gain = torch.empty_like(q_gain) if dq_gain is None else dq_gain
+    dq_gain = torch.empty_like(q_gain) if dq_gain is None and q_gain is not None else dq_gain
     dk_gain = torch.empty_like(k_gain) if dk_gain is None and k is not None and k_gain is not None else dk_gain
     shape, dev, rows, at = _heads(what, q, k, rotary, (("dq_out", dq_out), ("dq", dq)), (("dk_out", dk_out), ("dk", dk)))
     for name, t in (("q_gain", q_gain), ("dq_gain", dq_gain)) + ((("k_gain", k_gain), ("dk_gain", dk_gain)) if k is not None else ()):
