@@ -60,7 +60,6 @@ struct Blocks {
     int first, from, to;
     __device__ __forceinline__ int count() const { return first + to - from; }
     __device__ __forceinline__ int at(int i) const { return i < first ? i : from + i - first; }
-    __device__ __forceinline__ bool has(int block) const { return block < first || (block >= from && block < to); }
     __device__ __forceinline__ Blocks join(const Blocks& o) const {
         Blocks r;
         r.from = count() == 0 ? o.from : o.count() == 0 ? from : min(from, o.from);
