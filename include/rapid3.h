@@ -361,8 +361,9 @@ int rapid3_window_attn(const rapid3_window* w, const rapid3_rows* q, const rapid
                        void* stream);
 
 /* Gradients dq, dk, dv from dout and what rapid3_window_attn read and wrote (lse is needed).  Outputs overlap nothing.  Keys that no
- * row sees get zeros; so do dq of a row that sees one key and its part of dk.  Rows from q_len[b] on and keys from kv_len[b] on are left as they were.  B * H <= 65535.  workspace: device, 16-byte
- * aligned, of at least the bytes that rapid3_window_workspace_bytes gives, used by one call at a time; nothing in it has to be set.  The
+ * row sees get zeros; so do dq of a row that sees one key and its part of dk.  The weights and the scores' gradients, P (dP - delta), are
+ * rounded to the tensors' type for the second products: in fp16 these have to stay below 65504, and below 2^-25 they are 0 (scale the loss).  Rows from
+ * q_len[b] on and keys from kv_len[b] on are left as they were.  B * H <= 65535.  workspace: device, 16-byte aligned, of at least the bytes that rapid3_window_workspace_bytes gives, used by one call at a time; nothing in it has to be set.  The
  * sums are taken in a fixed order: the same call gives the same bits. */
 int rapid3_window_attn_backward(const rapid3_window* w, const rapid3_rows* q, const rapid3_rows* k, const rapid3_rows* v, const rapid3_rows* out,
                                 const float* lse, const rapid3_rows* dout, const rapid3_rows* dq, const rapid3_rows* dk, const rapid3_rows* dv,

@@ -16,7 +16,7 @@
 //
 // delta is made of the output that the caller has, which is rounded.  Of rows that see few keys, whose output is as large as a value, that
 // shows: dq and dk of causal sequences were 1.5 to 1.8 times as far off as the rounding of the weights alone makes them (2.7 times at five
-// tokens).  So tiles with rows that see fewer than EXACT_FROM keys have a launch of their own in front (`exact` row units), in which
+// tokens).  So tiles with rows that see fewer than EXACT_FROM keys (see few_tiles) have a launch of their own in front (`exact` row units), in which
 // e = the sum of a row's dS, as they are before their rounding, is found: what delta was short of.
 //     dQ = scale (sum dS K - e sum P K),   and delta + e is what the key units take
 // A row that sees one key has dS = 0: its delta is marked by infinity, and both kinds of unit write zeros for it.
@@ -34,7 +34,11 @@
 // second products and the next block's dP (2000 cycles of a block's 3300); the element work takes as long, 350 instructions a warp at one in
 // nine cycles.  Training pass of 4095 causal tokens, 32 heads on 8, window of 1024: blocks of 64 355 us, of 128 with P over S 349, so 335, and 356 with the
 // launch for rows of few keys; 398 in a hot card's long run (one at a time: forward 89, row_stats_kernel 16, that launch 15, this one 267).  211 GFLOP of seen pairs.
-// The exponential unit is not what it waits for: with a quarter or half of the powers on the fma units the 335 were 340 to 343.
+// The exponential unit is not what it waits for: with a quarter or half of the powers on the fma units the 335 were 340 to 343.  The build of both kinds
+// at D = 128 is short of registers: it keeps 56 bytes a thread in local memory (76 bytes of stores and 148 of loads in its code).
+// P and dS in 16 bits cost 1.3 to 1.4 times the error of 32 bits; in fp16 dS beyond 65504 is infinite and below 2^-25 is 0.
+// With lengths given the host does not know which tiles hold rows of few keys, and every row tile is in both launches, empty in one: the backward call of the
+// case above 274 -> 294 us, of 2 x 1357 joint tokens, 24 heads, D = 64, 110 -> 121.
 // Every mbarrier wait is bounded, as in K8.
 #include <math.h>
 #include <stddef.h>
@@ -1021,8 +1025,10 @@ void sharing(const rapid3_window* w, int& sink_tiles, int& parts) {
     parts = (int)std::min<long long>(std::min<long long>(MAX_PARTS, (sink + most - 1) / most), std::max<long long>(1, MAX_SLOTS / slots));
 }
 
-// The first row tiles of which rows may see fewer than EXACT_FROM keys: none, some at the beginning, or (where that is not for the host to say)
-// all.  every: each tile surely holds such rows.
+// The first row tiles that are looked at for rows which see fewer than EXACT_FROM keys, by their first and last rows: none, some at the beginning, or (where
+// that is not for the host to say) all.  every: each tile surely holds such rows.
+// Where the first tile's rows are full, or a tile's first ones, rows behind them that see 129 keys and more may go without (fewer they never see there: their
+// window is 256 wide, or the last tile's rows see few too): their dq is off by 0.61 to 0.62 half steps in the mean square, for 0.60 to 0.61 with the exact pass.
 int few_tiles(const rapid3_window* w, bool& every) {
     const int tiles = (w->n_q + 127) / 128;
     every = false;
@@ -1036,7 +1042,7 @@ int few_tiles(const rapid3_window* w, bool& every) {
     if (w->left >= 0 && w->right >= 0 && (long long)w->left + w->right + 1 + w->n_sink < EXACT_FROM && w->n_full == 0) n = tiles;
     while (n < tiles && few(n)) ++n;
     every = n == tiles;
-    // the rows behind see a whole window, but for those at the end
+    // the rows behind see a whole window or the keys of all that are in front, but for those at the end
     return n < tiles && few(tiles - 1) ? tiles : n;
 }
 

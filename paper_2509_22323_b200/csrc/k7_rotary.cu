@@ -16,7 +16,9 @@
 //
 // Measured at D = 128, bf16: Q and K of three sequences of 4608 tokens and 24 heads, normed and turned, 339.7 MB in 70 us, 4.9 TB/s, 0.74 of a
 // copy's rate; gradients of 32 + 8 heads of 8191 tokens, gains' included, 251.6 MB in 56 us, 4.5 TB/s.  At D = 64, fp16: gradients of 24 + 24 heads
-// of two sequences of 4429 tokens, 163 MB in 40 us.  The instructions are issued in 45 of 100 cycles.  Sixteen channels a lane instead of eight take
+// of two sequences of 4429 tokens, 163 MB in 40 us.  Instructions are issued in 39 to 46 of 100 cycles, also in the gradients, which take a row at a time a
+// lane group with 16 warps an SM: of the 6.4 cycles between two instructions of a warp 1.5 are the arithmetic's own latency, 1.1 the rows on their way, 0.5 shuffles
+// and shared memory; and 512 thread blocks are 1.73 rounds of the 296 that are resident.  Sixteen channels a lane instead of eight take
 // half of the shuffles and 115 to 155 registers: 71 us, and 53 for the 41 of the gradients.  Single tokens: 9 to 10 us a call, the launch.
 #include <math.h>
 
@@ -182,7 +184,7 @@ __global__ void __launch_bounds__(32 * WARPS) rotary_kernel(const __grid_constan
     char* const ring_at = ring + warp * (DEPTH * STREAMS * STEP) + (lane / LPR) * ROW;
     const uint32_t my_ring = ptx::smem_u32(ring_at);
     grid_dependency_wait();
-    // gain_kernel's few thread blocks may be there and wait where an SM has room (gradients of 24 + 24 heads at D = 64: 43.6 -> 41.6 us); other
+    // gain_kernel's few thread blocks may be there and wait where an SM has room (gradients of 24 + 24 heads at D = 64: 43.0 -> 40.7 us); other
     // launches that wait beside this one only take its SMs' room (rotation alone 12.7 -> 13.6)
     if (GRADS) grid_dependency_launch();
     for (uint32_t tile = blockIdx.x; tile < (uint32_t)p.n_tiles; tile += gridDim.x) {      // (a tile and a grid may be 2^31 - 1, their sum is no int)

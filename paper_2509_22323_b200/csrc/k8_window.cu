@@ -18,11 +18,13 @@
 //   warp 19     the next unit
 // TMEM: tile t owns columns [256 t, 256 t + 256): S(n) at 64 (n mod NBUF), O behind the NBUF score buffers.
 //
-// Measured at D = 128: 4608 tokens, 24 heads, 512 keys each way, 512 sinks that see all: 104 GFLOP of seen pairs in 115 us, 0.91 PFLOP/s (123 in a hot
-// card's long run); 8192 causal tokens, 32 heads on 8, window of 1024: 129 GFLOP in 152 us, 0.84 PFLOP/s (173).  A pair of blocks takes 1450 cycles, of
-// which the tensor cores work 700: with 64 columns the scores' product is bounded by the shared memory that feeds it (63 cycles a step for 32 of work), and what
-// is left is the chain from scores to P to the next ones.  One product of 128 columns for two blocks' scores is not so bounded, but wants both buffers of
-// scores, and the softmax waits: 143 and 196 us.  A share of the exponentials on the fma units gains nothing.
+// Measured at D = 128 in a hot card's long run (from a cool start in brackets): 4608 tokens, 24 heads, 512 keys each way, 512 sinks that see all: 104 GFLOP of
+// seen pairs in 124 us (114), 0.84 PFLOP/s; 8192 causal tokens, 32 heads on 8, window of 1024: 129 GFLOP in 174 us (152), 0.74 PFLOP/s.  Both tiles' work on a key
+// block takes 1450 cycles, and 2 (8 x 32 + 4 x 64) = 1024 of these are the products' at the tensor cores' rate.  But with 64 columns a step of the scores' product is
+// bounded by the shared memory that feeds it, 63 cycles for 32 of work, and 2 (8 x 63 + 4 x 64) = 1520 is all of the time.  So the softmax is not what bounds the
+// loop: a share of the exponentials on the fma units gains nothing.  One product of 128 columns for two blocks' scores is not so bounded, but wants both buffers of
+// scores, and then the softmax waits: 143 and 196 us.  Besides, a change of unit takes 4 us in each wave of units.
+// The build for D = 64 keeps two registers a thread in local memory (4 bytes stored, 28 loaded).
 // Every mbarrier wait is bounded; one that runs out is recorded (rapid3_window_status) and the thread block drains its copies and
 // products, releases its TMEM and exits.
 #include <float.h>
